@@ -1,0 +1,249 @@
+// Entry points of the sampling phase: argument checks on the host, then the launches on the caller's stream.  Nothing here
+// allocates device memory or synchronises; a plan is host data.
+#include <hip/hip_runtime_api.h>
+
+#include <cmath>
+#include <new>
+
+#include "paged.h"
+
+namespace {
+
+bool misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+int element_size(int32_t dtype) { return dtype == PA_BF16 ? 2 : 4; }
+
+int check_rope(const rope_axes_desc_t* d) {
+  if (!d) return PA_ERR_NULL;
+  if (d->head_dim < 2 || d->head_dim > 2 * PA_ROPE_MAX_PAIRS) return PA_ERR_SHAPE;
+  if (d->rotary_dim < 2 || d->rotary_dim > d->head_dim || d->rotary_dim % 2) return PA_ERR_SHAPE;
+  if (d->num_axes < 1 || d->num_axes > PA_ROPE_MAX_AXES) return PA_ERR_SHAPE;
+  if (d->layout != PA_ROPE_HALVES && d->layout != PA_ROPE_PAIRS) return PA_ERR_UNSUPPORTED;
+  for (int i = 0; i < d->rotary_dim / 2; ++i)
+    if (d->pair_axis[i] >= d->num_axes) return PA_ERR_SHAPE;
+  return PA_OK;
+}
+
+// `tokens` rows of `heads` heads, `stride` elements apart
+int check_rows(const void* p, int64_t stride, int32_t heads, int32_t D, int32_t dtype) {
+  if (!p) return PA_ERR_NULL;
+  if (stride < (int64_t)heads * D || stride > ((int64_t)1 << 40)) return PA_ERR_SHAPE;
+  if (misaligned(p, (uintptr_t)element_size(dtype))) return PA_ERR_ALIGN;
+  return PA_OK;
+}
+
+int rope_call(const rope_axes_desc_t* desc, int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+              int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads, const int32_t* positions, const float* inv_freq,
+              void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* hip_stream, float sign) {
+  int st = check_rope(desc);
+  if (st != PA_OK) return st;
+  if (dtype != PA_F32 && dtype != PA_BF16) return PA_ERR_UNSUPPORTED;
+  if (num_tokens < 0 || num_tokens > ((int64_t)1 << 31) - 1 || num_q_heads < 1 || num_q_heads > 65536 || num_k_heads < 0 ||
+      num_k_heads > 65536)
+    return PA_ERR_SHAPE;
+  if (num_tokens == 0) return PA_OK;
+  if (!positions || !inv_freq) return PA_ERR_NULL;
+  if ((st = check_rows(q, q_stride, num_q_heads, desc->head_dim, dtype)) != PA_OK) return st;
+  if ((st = check_rows(q_out, q_out_stride, num_q_heads, desc->head_dim, dtype)) != PA_OK) return st;
+  if (num_k_heads > 0) {
+    if ((st = check_rows(k, k_stride, num_k_heads, desc->head_dim, dtype)) != PA_OK) return st;
+    if ((st = check_rows(k_out, k_out_stride, num_k_heads, desc->head_dim, dtype)) != PA_OK) return st;
+  }
+  if (misaligned(positions, 4) || misaligned(inv_freq, 4)) return PA_ERR_ALIGN;
+  pa::RopeArgs a{};
+  a.rope = *desc;
+  a.dtype = dtype;
+  a.Hq = num_q_heads;
+  a.Hk = num_k_heads;
+  a.sign = sign;
+  a.T = num_tokens;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_out_stride = k_out_stride;
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  return pa::launch_rope(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
+}
+
+// What every call on a plan checks; `empty` is set when there is nothing to do.
+int check_call(const paged_attn_plan_t* plan, const int32_t* page_table, const int32_t* seq_lens, const int32_t* cu_new,
+               int32_t num_seqs, int64_t num_tokens, bool* empty) {
+  if (!plan) return PA_ERR_NULL;
+  const paged_attn_desc_t& d = plan->desc;
+  if (num_seqs < 0 || num_seqs > d.max_seqs || num_tokens < 0 || num_tokens > d.max_tokens) return PA_ERR_SHAPE;
+  *empty = num_seqs == 0 || num_tokens == 0;
+  if (*empty) return PA_OK;
+  if (!page_table || !seq_lens || !cu_new) return PA_ERR_NULL;
+  if (misaligned(page_table, 4) || misaligned(seq_lens, 4) || misaligned(cu_new, 4)) return PA_ERR_ALIGN;
+  return PA_OK;
+}
+
+// Host-only plans and other devices: after all other checks, so that those can be tested without a device.
+int check_device(const paged_attn_desc_t& d) {
+  if (d.device < 0) return PA_ERR_UNSUPPORTED;
+  int cur = -1;
+  return hipGetDevice(&cur) == hipSuccess && cur == d.device ? PA_OK : PA_ERR_HIP;  // the plan's device must be current
+}
+
+int append_call(const paged_attn_plan_t* plan, const rope_axes_desc_t* rope, const void* q, int64_t q_stride, const void* k,
+                int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions, const float* inv_freq,
+                void* q_out, int64_t q_out_stride, void* k_cache, void* v_cache, const int32_t* page_table,
+                const int32_t* seq_lens, const int32_t* cu_new, int32_t num_seqs, int64_t num_tokens, void* hip_stream) {
+  bool empty = false;
+  int st = check_call(plan, page_table, seq_lens, cu_new, num_seqs, num_tokens, &empty);
+  if (st != PA_OK || empty) return st;
+  const paged_attn_desc_t& d = plan->desc;
+  if ((st = check_rows(k, k_stride, d.num_kv_heads, d.head_dim, d.dtype)) != PA_OK) return st;
+  if ((st = check_rows(v, v_stride, d.num_kv_heads, d.head_dim, d.dtype)) != PA_OK) return st;
+  if (!k_cache || !v_cache) return PA_ERR_NULL;
+  if (misaligned(k_cache, 16) || misaligned(v_cache, 16)) return PA_ERR_ALIGN;
+  pa::RopeArgs a{};
+  if (rope) {
+    if (rope->head_dim != d.head_dim) return PA_ERR_SHAPE;
+    if (!positions || !inv_freq || !q != !q_out) return PA_ERR_NULL;
+    if (misaligned(positions, 4) || misaligned(inv_freq, 4)) return PA_ERR_ALIGN;
+    a.rope = *rope;
+    if (q) {
+      if ((st = check_rows(q, q_stride, d.num_q_heads, d.head_dim, d.dtype)) != PA_OK) return st;
+      if ((st = check_rows(q_out, q_out_stride, d.num_q_heads, d.head_dim, d.dtype)) != PA_OK) return st;
+      a.Hq = d.num_q_heads;
+    }
+  } else {
+    a.rope.head_dim = d.head_dim;
+    a.rope.layout = PA_ROPE_HALVES;
+  }
+  if ((st = check_device(d)) != PA_OK) return st;
+  a.dtype = d.dtype;
+  a.Hk = a.Hv = d.num_kv_heads;
+  a.sign = 1.f;
+  a.T = num_tokens;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out_stride = q_out_stride;
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.page_table = page_table;
+  a.seq_lens = seq_lens;
+  a.cu_new = cu_new;
+  a.B = num_seqs;
+  a.table_width = d.max_pages_per_seq;
+  a.page_shift = plan->page_shift;
+  a.num_pages = d.num_pages;
+  return pa::launch_append(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rope_axes_forward(const rope_axes_desc_t* desc, int32_t dtype, const void* q, int64_t q_stride, const void* k,
+                      int64_t k_stride, int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
+                      const int32_t* positions, const float* inv_freq, void* q_out, int64_t q_out_stride, void* k_out,
+                      int64_t k_out_stride, void* hip_stream) {
+  return rope_call(desc, dtype, q, q_stride, k, k_stride, num_tokens, num_q_heads, num_k_heads, positions, inv_freq, q_out,
+                   q_out_stride, k_out, k_out_stride, hip_stream, 1.f);
+}
+
+int rope_axes_backward(const rope_axes_desc_t* desc, int32_t dtype, const void* q, int64_t q_stride, const void* k,
+                       int64_t k_stride, int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
+                       const int32_t* positions, const float* inv_freq, void* q_out, int64_t q_out_stride, void* k_out,
+                       int64_t k_out_stride, void* hip_stream) {
+  return rope_call(desc, dtype, q, q_stride, k, k_stride, num_tokens, num_q_heads, num_k_heads, positions, inv_freq, q_out,
+                   q_out_stride, k_out, k_out_stride, hip_stream, -1.f);
+}
+
+int paged_attn_plan(const paged_attn_desc_t* desc, paged_attn_plan_t** plan_out, size_t* workspace_bytes_out) {
+  if (plan_out) *plan_out = nullptr;
+  if (!desc || !plan_out || !workspace_bytes_out) return PA_ERR_NULL;
+  const paged_attn_desc_t& d = *desc;
+  if (d.num_q_heads < 1 || d.num_kv_heads < 1 || d.num_q_heads % d.num_kv_heads || d.num_q_heads > 4096) return PA_ERR_SHAPE;
+  if (d.num_pages < 1 || d.num_pages > ((int64_t)1 << 31) - 1) return PA_ERR_SHAPE;
+  if (d.max_seqs < 1 || d.max_seqs > 65536 || d.max_tokens < 1 || d.max_tokens > (1 << 24)) return PA_ERR_SHAPE;
+  if (!(d.softmax_scale > 0.0f) || !std::isfinite(d.softmax_scale) || d.device < -1) return PA_ERR_SHAPE;
+  if (d.max_pages_per_seq < 1 || d.page_size < 1) return PA_ERR_SHAPE;
+  if (d.head_dim != 64 && d.head_dim != 128) return PA_ERR_UNSUPPORTED;
+  if (d.dtype != PA_F32 && d.dtype != PA_BF16) return PA_ERR_UNSUPPORTED;
+  if (d.page_size < 16 || d.page_size > 1024 || (d.page_size & (d.page_size - 1))) return PA_ERR_UNSUPPORTED;
+  if ((int64_t)d.max_pages_per_seq * d.page_size > ((int64_t)1 << 30)) return PA_ERR_SHAPE;
+  paged_attn_plan_t* p = new (std::nothrow) paged_attn_plan_t;
+  if (!p) return PA_ERR_ALLOC;
+  p->desc = d;
+  while ((1 << p->page_shift) < d.page_size) ++p->page_shift;
+  p->ws_bytes = 256;
+  *plan_out = p;
+  *workspace_bytes_out = p->ws_bytes;
+  return PA_OK;
+}
+
+void paged_attn_destroy(paged_attn_plan_t* plan) { delete plan; }
+
+int paged_kv_append(const paged_attn_plan_t* plan, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                    void* k_cache, void* v_cache, const int32_t* page_table, const int32_t* seq_lens, const int32_t* cu_new,
+                    int32_t num_seqs, int64_t num_tokens, void* hip_stream) {
+  return append_call(plan, nullptr, nullptr, 0, k, k_stride, v, v_stride, nullptr, nullptr, nullptr, 0, k_cache, v_cache,
+                     page_table, seq_lens, cu_new, num_seqs, num_tokens, hip_stream);
+}
+
+int paged_kv_append_rope(const paged_attn_plan_t* plan, const rope_axes_desc_t* rope, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                         const float* inv_freq, void* q_out, int64_t q_out_stride, void* k_cache, void* v_cache,
+                         const int32_t* page_table, const int32_t* seq_lens, const int32_t* cu_new, int32_t num_seqs,
+                         int64_t num_tokens, void* hip_stream) {
+  const int st = check_rope(rope);
+  if (st != PA_OK) return st;
+  return append_call(plan, rope, q, q_stride, k, k_stride, v, v_stride, positions, inv_freq, q_out, q_out_stride, k_cache,
+                     v_cache, page_table, seq_lens, cu_new, num_seqs, num_tokens, hip_stream);
+}
+
+int paged_attn_forward(const paged_attn_plan_t* plan, const void* q, int64_t q_stride, const void* k_cache,
+                       const void* v_cache, const int32_t* page_table, const int32_t* seq_lens, const int32_t* cu_new,
+                       int32_t num_seqs, int64_t num_tokens, const int32_t* shared_len, void* out, float* lse_out,
+                       void* workspace, size_t workspace_bytes, void* hip_stream) {
+  bool empty = false;
+  int st = check_call(plan, page_table, seq_lens, cu_new, num_seqs, num_tokens, &empty);
+  if (st != PA_OK || empty) return st;
+  const paged_attn_desc_t& d = plan->desc;
+  if ((st = check_rows(q, q_stride, d.num_q_heads, d.head_dim, d.dtype)) != PA_OK) return st;
+  if (!k_cache || !v_cache || !out || !workspace) return PA_ERR_NULL;
+  if (misaligned(q, 16) || q_stride * element_size(d.dtype) % 16 || misaligned(k_cache, 16) || misaligned(v_cache, 16) ||
+      misaligned(out, 16) || misaligned(workspace, 16) || misaligned(lse_out, 4) || misaligned(shared_len, 4))
+    return PA_ERR_ALIGN;
+  if (workspace_bytes < plan->ws_bytes) return PA_ERR_WORKSPACE;
+  if ((st = check_device(d)) != PA_OK) return st;
+  pa::PagedArgs a{};
+  a.q = q;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.out = out;
+  a.lse = lse_out;
+  a.page_table = page_table;
+  a.seq_lens = seq_lens;
+  a.cu_new = cu_new;
+  a.q_stride = q_stride;
+  a.num_pages = d.num_pages;
+  a.dtype = d.dtype;
+  a.B = num_seqs;
+  a.T = (int32_t)num_tokens;
+  a.Hq = d.num_q_heads;
+  a.Hkv = d.num_kv_heads;
+  a.D = d.head_dim;
+  a.group = d.num_q_heads / d.num_kv_heads;
+  a.table_width = d.max_pages_per_seq;
+  a.page_shift = plan->page_shift;
+  a.scale = d.softmax_scale;
+  return pa::launch_paged_attn(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,186 @@
+"""Sampling phase on the CPU: the exported symbols, what the plan and the calls refuse (host-only plans; nothing is launched), and pins of the
+float64 definitions that the GPU tests compare with."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+import paper_2507_07966_amd as pa
+from oracle import ref_attention, ref_sampling as ref
+from paper_2507_07966_amd import binding, sampling
+from tests.sampling_util import Paged
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_library_exports_every_declared_symbol():
+    header = open(os.path.join(ROOT, "include", "paged_attn.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = set(re.findall(r"\b((?:paged|rope)_\w+)\s*\(", header))
+    lib = ctypes.CDLL(binding.library_path())
+    assert declared == set(sampling.EXPORTED_SYMBOLS)
+    for name in declared:
+        assert hasattr(lib, name), name
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(num_q_heads=0), 2), (dict(num_kv_heads=3), 2), (dict(head_dim=96), 3), (dict(page_size=8), 3), (dict(page_size=48), 3),
+    (dict(page_size=2048), 3), (dict(num_pages=0), 2), (dict(num_pages=1 << 31), 2), (dict(max_pages_per_seq=0), 2),
+    (dict(max_pages_per_seq=1 << 27), 2), (dict(max_seqs=0), 2), (dict(max_seqs=65537), 2), (dict(max_tokens=0), 2),
+    (dict(max_tokens=(1 << 24) + 1), 2), (dict(softmax_scale=0.0), 2), (dict(softmax_scale=float("nan")), 2), (dict(device=-2), 2),
+    (dict(dtype="f16"), 3), (dict(num_q_heads=1 << 40), 2),
+])
+def test_plan_refuses(kw, status):
+    args = dict(num_q_heads=28, num_kv_heads=4, head_dim=128, page_size=64, num_pages=100, max_pages_per_seq=20, max_seqs=8,
+                max_tokens=64, softmax_scale=0.1, dtype="bf16", device=-1)
+    with pytest.raises(pa.PrefixAttnError) as e:
+        pa.paged_attn_plan(**{**args, **kw})
+    assert e.value.status == status
+
+
+@pytest.mark.parametrize("args,kw", [(((),), {}), (((1, 2, 3, 4, 22),), {}), (((30,),), {}), (((-1, 33),), {}), (((32,),), dict(layout="rows")),
+                                     (((40,),), dict(rotary_dim=80)), (((0,),), dict(rotary_dim=0))])
+def test_rope_axes_refuses(args, kw):
+    with pytest.raises(pa.PrefixAttnError):
+        pa.rope_axes(*args, 64, **kw)
+
+
+def test_axes_of_pairs():
+    assert pa.rope_axes((2, 1, 1), 8).pair_axis == (0, 0, 1, 2)
+    assert pa.rope_axes((1, 3, 2), 16, rotary_dim=12, interleaved=True).pair_axis == (0, 1, 2, 1, 2, 1)
+
+
+def raw(plan, call, **kw):
+    """A call of the C ABI with plausible pointers; nothing of it is read, since every case is refused or the plan is host-only."""
+    lib = sampling._load()
+    p = 1 << 20
+    a = dict(q=p, qs=28 * 128, k=p, ks=4 * 128, v=p, vs=4 * 128, pos=p, freq=p, qo=p, qos=28 * 128, kc=p, vc=p, table=p, lens=p, cu=p, seqs=4, tokens=4,
+             shared=None, out=p, lse=p, ws=p, bytes=1 << 40, rope=pa.rope_axes((64,), 128)._ref)
+    a.update(kw)
+    g = lambda names: [a[n] for n in names.split()]
+    if call == "append":
+        return lib.paged_kv_append(plan, *g("k ks v vs kc vc table lens cu seqs tokens"), None)
+    if call == "rope":
+        return lib.paged_kv_append_rope(plan, *g("rope q qs k ks v vs pos freq qo qos kc vc table lens cu seqs tokens"), None)
+    return lib.paged_attn_forward(plan, *g("q qs kc vc table lens cu seqs tokens shared out lse ws bytes"), None)
+
+
+def test_calls_check_their_arguments_before_launch():
+    plan = pa.paged_attn_plan(28, 4, 128, 64, 100, 20, 8, 64, 0.1, device=-1)
+    h = plan.handle
+    for call in ("append", "rope", "attend"):
+        assert raw(None, call) == 1
+        assert raw(h, call) == 3                                   # all arguments are fine, but the plan is host-only
+        assert raw(h, call, tokens=0) == 0 and raw(h, call, seqs=0) == 0
+        for name, status in (("seqs", 2), ("tokens", 2)):
+            assert raw(h, call, **{name: -1}) == status and raw(h, call, **{name: 65}) == status
+        for name in ("kc", "vc", "table", "lens", "cu"):
+            assert raw(h, call, **{name: None}) == 1, (call, name)
+            assert raw(h, call, **{name: (1 << 20) + 2}) == 4, (call, name)
+    for name in ("k", "v"):
+        assert raw(h, "append", **{name: None}) == 1 and raw(h, "append", **{name + "s": 511}) == 2
+        assert raw(h, "append", **{name: (1 << 20) + 1}) == 4
+    assert raw(h, "rope", q=None) == 1 and raw(h, "rope", qo=None) == 1 and raw(h, "rope", q=None, qo=None) == 3
+    assert raw(h, "rope", pos=None) == 1 and raw(h, "rope", freq=None) == 1 and raw(h, "rope", rope=None) == 1
+    assert raw(h, "rope", rope=pa.rope_axes((32,), 64)._ref) == 2 and raw(h, "rope", qs=28 * 128 - 1) == 2
+    for name in ("q", "out", "ws"):
+        assert raw(h, "attend", **{name: None}) == 1 and raw(h, "attend", **{name: (1 << 20) + 8}) == 4
+    assert raw(h, "attend", lse=None) == 3 and raw(h, "attend", lse=(1 << 20) + 2) == 4 and raw(h, "attend", shared=(1 << 20) + 2) == 4
+    assert raw(h, "attend", qs=28 * 128 + 4) == 4 and raw(h, "attend", qs=28 * 128 + 8) == 3
+    assert raw(h, "attend", bytes=plan.workspace_bytes - 1) == 5
+    plan.destroy()
+    with pytest.raises(ValueError):
+        plan.handle
+
+
+def test_rope_checks_its_arguments_before_launch():
+    lib, p = sampling._load(), 1 << 20
+    desc = pa.rope_axes((20, 12), 64)._desc
+
+    def call(d=desc, dtype=1, q=p, qs=256, k=p, ks=128, tokens=3, hq=4, hk=2, pos=p, freq=p, qo=p, qos=256, ko=p, kos=128):
+        return lib.rope_axes_forward(ctypes.byref(d) if d else None, dtype, q, qs, k, ks, tokens, hq, hk, pos, freq, qo, qos, ko, kos, None)
+
+    def changed(**kw):
+        d = sampling._RopeDesc.from_buffer_copy(desc)
+        for n, v in kw.items():
+            setattr(d, n, v)
+        return d
+
+    assert call(tokens=0) == 0 and call(d=None) == 1 and call(dtype=2) == 3
+    for kw in (dict(tokens=-1), dict(hq=0), dict(hk=-1), dict(qs=255), dict(kos=127)):
+        assert call(**kw) == 2, kw
+    for name in ("q", "k", "pos", "freq", "qo", "ko"):
+        assert call(**{name: None}) == 1 and call(**{name: p + 1}) == 4, name
+    for kw, st in ((dict(head_dim=0), 2), (dict(head_dim=258), 2), (dict(rotary_dim=66), 2), (dict(rotary_dim=33), 2), (dict(num_axes=1), 2),
+                   (dict(num_axes=5), 2), (dict(layout=2), 3)):
+        assert call(d=changed(**kw)) == st, kw
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    import torch
+    x = Paged("bf16", (4, 2), 64, 16, [40, 3], [2, 1])
+    plan = x.plan(device=-1)     # a host-only plan checks tensors on the CPU
+    t = lambda a, dt=None: torch.from_numpy(np.ascontiguousarray(a)) if dt is None else torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(dt)
+    good = dict(q=t(x.q, torch.bfloat16), k_cache=t(x.k, torch.bfloat16), v_cache=t(x.v, torch.bfloat16), page_table=t(x.table),
+                seq_lens=t(x.lens), cu_new=t(x.cu), out=torch.zeros(3, 4, 64, dtype=torch.bfloat16), lse_out=torch.zeros(4, 3),
+                workspace=torch.empty(max(16, plan.workspace_bytes), dtype=torch.uint8))
+
+    def status(**kw):
+        with pytest.raises(pa.PrefixAttnError) as e:
+            pa.paged_attn_forward(plan, **{**good, **kw}, stream=1)
+        return e.value.status
+
+    assert status() == 3                                                   # host-only
+    assert status(q=good["q"].float()) == 3 and status(q=good["q"][:, :2]) == 2 and status(q=good["q"].transpose(0, 1)) == 2
+    assert status(q=good["q"][:, :, ::2]) == 2 and status(k_cache=good["k_cache"][1:]) == 2 and status(v_cache=good["v_cache"].transpose(1, 2)) == 2
+    assert status(page_table=good["page_table"].long()) == 3 and status(page_table=good["page_table"][:, 1:]) == 2
+    assert status(seq_lens=good["seq_lens"][:1]) == 2 and status(cu_new=good["cu_new"][:2]) == 2
+    assert status(out=good["out"].float()) == 3 and status(out=good["out"][:2]) == 2 and status(lse_out=good["lse_out"].T) == 2
+    assert status(shared_len=torch.zeros(1)) == 3 and status(shared_len=torch.zeros(2, dtype=torch.int32)) == 2
+    assert status(workspace=torch.empty(1, dtype=torch.uint8)) in (4, 5)
+    with pytest.raises(pa.PrefixAttnError):
+        pa.paged_kv_append(plan, good["q"][:, :2], good["q"], *[good[n] for n in ("k_cache", "v_cache", "page_table", "seq_lens", "cu_new")])
+    plan.destroy()
+
+
+# ---- pins of the definitions ----
+
+def test_rope_definition_turns_pairs_and_keeps_products():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((5, 3, 10))
+    freq = np.array([1.0, 0.5, 0.25, 2.0], dtype=np.float32)
+    pos = np.array([[0, 1, 2, 3, 4], [0, 0, 7, 0, -7]])
+    axis = (0, 1, 1, 0)
+    for layout in ("halves", "pairs"):
+        y = ref.rope(x, pos, freq, axis, layout)
+        assert np.array_equal(y[0], x[0]) and np.array_equal(y[:, :, 8:], x[:, :, 8:])
+        assert np.allclose((y ** 2).sum(-1), (x ** 2).sum(-1))
+        assert np.allclose(ref.rope(y, pos, freq, axis, layout, -1.0), x)
+        # <turned by p, turned by p + d> depends on d alone
+        a, b = ref.rope(x[:1], pos[:, 2:3], freq, axis, layout), ref.rope(x[1:2], pos[:, 3:4], freq, axis, layout)
+        c, d = ref.rope(x[:1], pos[:, 2:3] + 100, freq, axis, layout), ref.rope(x[1:2], pos[:, 3:4] + 100, freq, axis, layout)
+        assert np.allclose((a * b).sum(-1), (c * d).sum(-1))
+    # a hand-worked quarter turn: position 1, frequency pi / 2
+    q = ref.rope(np.array([[[3.0, 4.0]]]), np.array([[1]]), np.array([np.pi / 2]), (0,), "pairs")
+    assert np.allclose(q, [[[-4.0, 3.0]]])
+
+
+def test_paged_attention_definition_is_causal_attention_of_the_gathered_sequence():
+    x = Paged("f32", (6, 2), 64, 16, [40, 19], [40, 19], seed=1)
+    out, lse, mass, reach, keys = x.oracle()
+    k = np.concatenate([np.concatenate([x.k[p].transpose(1, 0, 2) for p in x.table[b] if p >= 0])[:n] for b, n in enumerate(x.lens)])
+    v = np.concatenate([np.concatenate([x.v[p].transpose(1, 0, 2) for p in x.table[b] if p >= 0])[:n] for b, n in enumerate(x.lens)])
+    empty = np.zeros((0, 2, 64))
+    want = ref_attention.prefix_shared_attention(x.q, empty, empty, k, v, x.lens, x.scale)
+    assert np.allclose(out, want[0], atol=1e-12) and np.allclose(lse, want[1], atol=1e-12)
+    assert (mass >= np.abs(out) - 1e-12).all() and list(keys[:3]) == [1, 2, 3]
+    # appended in pieces, the cache is the same
+    c = np.zeros_like(x.k)
+    lens1, cu1 = np.array([25, 0]), np.array([0, 25, 25])
+    c = ref.append(c, k[:25], x.table, lens1, cu1)
+    c = ref.append(c, np.concatenate([k[25:40], k[40:59]]), x.table, x.lens, np.array([0, 15, 34]))
+    for b, n in enumerate(x.lens):
+        for j in range(n):
+            assert np.array_equal(c[x.table[b, j // 16], :, j % 16], x.k[x.table[b, j // 16], :, j % 16])
