@@ -85,7 +85,7 @@ typedef struct {
   int64_t num_pages;         /* pages of the cache, 1 ... 2^31 - 1 */
   int32_t max_pages_per_seq; /* columns of the page table; times page_size at most 2^30 tokens */
   int32_t max_seqs;          /* most sequences of a call, 1 ... 65,536 */
-  int64_t max_tokens;        /* most packed rows of a call, 1 ... 2^24 */
+  int64_t max_tokens;        /* most packed rows of a call, 1 ... 2^24; times Hq below 2^31 */
   float softmax_scale;       /* finite and > 0 */
   int32_t dtype;             /* pa_dtype_t of q, k, v, the caches and out */
   int32_t device;            /* HIP device ordinal; -1 = host-only plan (validation and schedule only) */

@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "paged_attn.h"
+#include "paged_sched.h"
 
 namespace pa {
 
@@ -29,22 +30,49 @@ struct RopeArgs {
 int launch_rope(const RopeArgs& a, void* stream);
 int launch_append(const RopeArgs& a, void* stream);
 
+// A block whose keys were cut into pieces: pieces first .. last (numbers of shares) cover it.
+struct PagedCut {
+  int32_t token0, tokens, head, block;  // as in Segment and Piece; tokens 0: the share begins no block that it does not end
+  int32_t first, last;
+};
+// What workgroup 0 tells the merge about the line.
+struct PagedLine {
+  int64_t share;
+  int32_t active, shared;
+};
+
 struct PagedArgs {
   const void *q, *k_cache, *v_cache;
   void* out;
   float* lse;  // [Hq, T] or null
-  const int32_t *page_table, *seq_lens, *cu_new;
+  const int32_t *page_table, *seq_lens, *cu_new, *shared_len;
   int64_t q_stride;  // elements
   int64_t num_pages;
-  int32_t dtype, B, T, Hq, Hkv, D, group, table_width, page_shift;
+  int32_t dtype, D, Hq, table_width, page_shift;
   float scale;
+  PagedShape shape;        // `shared` is read on the device
+  int32_t groups, xcds;    // workgroups, and over how many XCDs they are laid out
+  int32_t blocks16;        // 16-row blocks of an item
+  // workspace
+  PagedLine* line;
+  int64_t* seg_start;      // [B + 2] cost at which segment i begins (with shared keys only: segment 0 is theirs)
+  PagedCut* cuts;          // [groups]
+  float* slots;            // [2 * groups][block_rows][D] fp32 partial outputs: of the block that share i continues (2 i) and
+  float* slot_lse;         //   of the one that it begins and does not end (2 i + 1); [2 * groups][block_rows]
+  float* rows;             // with shared keys, [2][T * Hq][D]: partials of whole blocks, own keys and shared ones
+  float* rows_lse;         // [2][T * Hq]
 };
-int launch_paged_attn(const PagedArgs& a, void* stream);
+int launch_paged_rows(const PagedArgs& a, void* stream);   // calls of few rows a sequence, and fp32
+int paged_rows_tile_keys(int32_t dtype, int32_t D);        // keys that its wavefronts share out in a step
+int launch_paged_merge(const PagedArgs& a, void* stream);
 
 }  // namespace pa
 
 struct paged_attn_plan {
   paged_attn_desc_t desc;
   int32_t page_shift = 0;
-  size_t ws_bytes = 0;
+  int32_t num_cu = 256, num_xcd = 8;
+  int32_t group = 1;
+  // workspace: byte offsets
+  size_t off_seg_start = 0, off_cuts = 0, off_slot_lse = 0, off_slots = 0, off_rows_lse = 0, off_rows = 0, ws_bytes = 0;
 };

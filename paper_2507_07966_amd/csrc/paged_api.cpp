@@ -144,6 +144,61 @@ int append_call(const paged_attn_plan_t* plan, const rope_axes_desc_t* rope, con
   return pa::launch_append(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
 }
 
+// Rows of a block for an average of `rows` rows a sequence (with shared keys: rows in all, which their blocks hold together).
+int32_t blocks16_for(int64_t rows, int32_t dtype) { return rows <= 16 ? 1 : rows <= 32 || dtype == PA_F32 ? 2 : 4; }
+
+// A call of at most this many rows a sequence is one of few rows: only such calls use shared_len.
+constexpr int64_t FEW_ROWS = 64;
+
+// A block's start and end cost about as much as this many keys, and a share of fewer keys is not worth a workgroup and a merge.
+constexpr int32_t START_KEYS = 64, MIN_SHARE = 256;
+
+pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                      const int32_t* page_table, const int32_t* seq_lens, const int32_t* cu_new, int32_t num_seqs, int32_t num_tokens,
+                      const int32_t* shared_len, void* out, float* lse_out, char* ws) {
+  const paged_attn_desc_t& d = plan.desc;
+  pa::PagedArgs a{};
+  a.q = q;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.out = out;
+  a.lse = lse_out;
+  a.page_table = page_table;
+  a.seq_lens = seq_lens;
+  a.cu_new = cu_new;
+  a.q_stride = q_stride;
+  a.num_pages = d.num_pages;
+  a.dtype = d.dtype;
+  a.D = d.head_dim;
+  a.Hq = d.num_q_heads;
+  a.table_width = d.max_pages_per_seq;
+  a.page_shift = plan.page_shift;
+  a.scale = d.softmax_scale;
+  const int64_t rows = (int64_t)num_tokens * plan.group;
+  a.shared_len = rows <= FEW_ROWS * num_seqs ? shared_len : nullptr;
+  a.blocks16 = blocks16_for(a.shared_len ? rows : (rows + num_seqs - 1) / num_seqs, d.dtype);
+  a.groups = plan.num_cu;
+  a.xcds = plan.num_xcd;
+  pa::PagedShape& s = a.shape;
+  s.B = num_seqs;
+  s.T = num_tokens;
+  s.Hkv = d.num_kv_heads;
+  s.group = plan.group;
+  s.block_rows = 16 * a.blocks16;
+  s.tile_keys = pa::paged_rows_tile_keys(d.dtype, d.head_dim);
+  s.capacity = d.max_pages_per_seq << plan.page_shift;
+  s.start_keys = START_KEYS;
+  s.min_share = MIN_SHARE;
+  a.line = reinterpret_cast<pa::PagedLine*>(ws);
+  a.seg_start = reinterpret_cast<int64_t*>(ws + plan.off_seg_start);
+  a.cuts = reinterpret_cast<pa::PagedCut*>(ws + plan.off_cuts);
+  a.slot_lse = reinterpret_cast<float*>(ws + plan.off_slot_lse);
+  a.slots = reinterpret_cast<float*>(ws + plan.off_slots);
+  a.rows_lse = reinterpret_cast<float*>(ws + plan.off_rows_lse);
+  a.rows = reinterpret_cast<float*>(ws + plan.off_rows);
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -171,6 +226,7 @@ int paged_attn_plan(const paged_attn_desc_t* desc, paged_attn_plan_t** plan_out,
   if (d.num_q_heads < 1 || d.num_kv_heads < 1 || d.num_q_heads % d.num_kv_heads || d.num_q_heads > 4096) return PA_ERR_SHAPE;
   if (d.num_pages < 1 || d.num_pages > ((int64_t)1 << 31) - 1) return PA_ERR_SHAPE;
   if (d.max_seqs < 1 || d.max_seqs > 65536 || d.max_tokens < 1 || d.max_tokens > (1 << 24)) return PA_ERR_SHAPE;
+  if (d.max_tokens * d.num_q_heads > ((int64_t)1 << 31) - 1) return PA_ERR_SHAPE;  // rows are numbered in 32 bits
   if (!(d.softmax_scale > 0.0f) || !std::isfinite(d.softmax_scale) || d.device < -1) return PA_ERR_SHAPE;
   if (d.max_pages_per_seq < 1 || d.page_size < 1) return PA_ERR_SHAPE;
   if (d.head_dim != 64 && d.head_dim != 128) return PA_ERR_UNSUPPORTED;
@@ -181,7 +237,33 @@ int paged_attn_plan(const paged_attn_desc_t* desc, paged_attn_plan_t** plan_out,
   if (!p) return PA_ERR_ALLOC;
   p->desc = d;
   while ((1 << p->page_shift) < d.page_size) ++p->page_shift;
-  p->ws_bytes = 256;
+  p->group = d.num_q_heads / d.num_kv_heads;
+  if (d.device >= 0) {
+    int n = 0;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, d.device) != hipSuccess || n < 1) {
+      (void)hipGetLastError();
+      delete p;
+      return PA_ERR_HIP;
+    }
+    p->num_cu = n;
+    p->num_xcd = n == 256 ? 8 : 1;  // the layout that shares are spread over XCDs for
+  }
+  // What the shares leave of blocks that they cut, and, where shared keys are a segment of their own, partials of all rows.
+  const int64_t block_rows = 64, slots = 2 * (int64_t)p->num_cu * block_rows;
+  const int64_t few = FEW_ROWS * d.max_seqs / p->group, tokens = few < d.max_tokens ? few : d.max_tokens;
+  size_t at = 256;
+  auto take = [&](size_t bytes) {
+    const size_t off = at;
+    at += (bytes + 255) / 256 * 256;
+    return off;
+  };
+  p->off_seg_start = take(((size_t)d.max_seqs + 2) * sizeof(int64_t));
+  p->off_cuts = take((size_t)p->num_cu * sizeof(pa::PagedCut));
+  p->off_slot_lse = take((size_t)slots * sizeof(float));
+  p->off_slots = take((size_t)slots * d.head_dim * sizeof(float));
+  p->off_rows_lse = take((size_t)tokens * d.num_q_heads * 2 * sizeof(float));
+  p->off_rows = take((size_t)tokens * d.num_q_heads * 2 * d.head_dim * sizeof(float));
+  p->ws_bytes = at;
   *plan_out = p;
   *workspace_bytes_out = p->ws_bytes;
   return PA_OK;
@@ -222,28 +304,10 @@ int paged_attn_forward(const paged_attn_plan_t* plan, const void* q, int64_t q_s
     return PA_ERR_ALIGN;
   if (workspace_bytes < plan->ws_bytes) return PA_ERR_WORKSPACE;
   if ((st = check_device(d)) != PA_OK) return st;
-  pa::PagedArgs a{};
-  a.q = q;
-  a.k_cache = k_cache;
-  a.v_cache = v_cache;
-  a.out = out;
-  a.lse = lse_out;
-  a.page_table = page_table;
-  a.seq_lens = seq_lens;
-  a.cu_new = cu_new;
-  a.q_stride = q_stride;
-  a.num_pages = d.num_pages;
-  a.dtype = d.dtype;
-  a.B = num_seqs;
-  a.T = (int32_t)num_tokens;
-  a.Hq = d.num_q_heads;
-  a.Hkv = d.num_kv_heads;
-  a.D = d.head_dim;
-  a.group = d.num_q_heads / d.num_kv_heads;
-  a.table_width = d.max_pages_per_seq;
-  a.page_shift = plan->page_shift;
-  a.scale = d.softmax_scale;
-  return pa::launch_paged_attn(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
+  const pa::PagedArgs a = arrange(*plan, q, q_stride, k_cache, v_cache, page_table, seq_lens, cu_new, num_seqs, (int32_t)num_tokens,
+                                  shared_len, out, lse_out, static_cast<char*>(workspace));
+  if (pa::launch_paged_rows(a, hip_stream) != 0) return PA_ERR_HIP;
+  return pa::launch_paged_merge(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
 }
 
 }  // extern "C"

@@ -1,0 +1,213 @@
+// Device side of the schedule of paged_sched.h, and small helpers of the kernels that attend over pages.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "mfma_tiles.h"
+#include "paged.h"
+
+namespace pa {
+
+// Exchange between lane l and lane l^32 (v_permlane32_swap; the results are read through named temporaries, as in the
+// prefill kernels), and reductions over the four lanes l, l^16, l^32, l^48 that hold one query column.
+__device__ inline void pair_exchange(float x, float& lo, float& hi) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const unsigned r0 = r[0], r1 = r[1];
+  lo = __uint_as_float(r0);
+  hi = __uint_as_float(r1);
+}
+__device__ inline float quad_max(float x) {
+  float a, b;
+  pair_exchange(fmaxf(x, __shfl_xor(x, 16)), a, b);
+  return fmaxf(a, b);
+}
+__device__ inline float quad_sum(float x) {
+  float a, b;
+  pair_exchange(x + __shfl_xor(x, 16), a, b);
+  return a + b;
+}
+
+// Wait until at most N of this wavefront's vector memory operations are under way (loads to LDS complete in order), or until its
+// reads of LDS have returned.  The compiler keeps memory accesses on their side of it.
+template <int N>
+__device__ inline void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ inline void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ inline int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// Lengths, tables and the like: nothing writes them while a kernel runs, which the address space says, so that uniform reads are scalar.
+__device__ inline int32_t read_const(const int32_t* p, int64_t i) {
+  typedef const __attribute__((address_space(4))) int32_t* Const;
+  return ((Const)p)[i];
+}
+
+// Where a row of a block's result goes: the call's output, or an fp32 partial.
+struct Place {
+  void* row;
+  float* lse;
+  bool partial;
+};
+template <typename T>
+__device__ inline void write_row(const Place& p, int ch, mt::f32x4 v) {
+  if (p.partial) {
+    *reinterpret_cast<mt::f32x4*>(static_cast<float*>(p.row) + ch) = v;
+  } else {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<T4*>(static_cast<T*>(p.row) + ch) = __builtin_convertvector(v, T4);
+  }
+}
+
+__device__ inline int32_t shared_keys(const PagedArgs& a) {
+  if (!a.shared_len) return 0;
+  return (int32_t)clamp64(read_const(a.shared_len, 0), 0, a.shape.capacity) & ~((1 << a.page_shift) - 1);  // whole pages
+}
+__device__ inline Segment load_segment(const PagedArgs& a, const PagedShape& s, int i) {
+  const int with = a.shared_len ? 1 : 0;
+  if (i < with) return shared_segment(s, read_const(a.cu_new, s.B));
+  return own_segment(s, read_const(a.cu_new, i - with), read_const(a.cu_new, i - with + 1), read_const(a.seq_lens, i - with));
+}
+
+// A workgroup's way along its share: one piece of a block at a time.  All members are uniform.
+struct Walk {
+  PagedShape shape;
+  Segment seg;
+  int32_t seg_index, segments, head, block;
+  int32_t table_row;   // of the page table
+  int32_t first_seq;   // the first sequence with new tokens: shared keys are read through its row
+  int32_t position;    // number of the share
+  bool shared;         // the segment is that of the shared keys
+  int64_t seg_start, x, x_end, share;
+
+  __device__ int64_t begin() const { return seg_start + head * seg.cost + blocks_cost(seg, block); }
+  __device__ int64_t end() const { return begin() + seg.first_cost + block * seg.more_cost; }
+  __device__ bool more() const { return x < x_end; }
+  __device__ void enter(const PagedArgs& a) {
+    shared = a.shared_len && seg_index == 0;
+    table_row = shared ? first_seq : seg_index - (a.shared_len ? 1 : 0);
+  }
+  __device__ Piece piece() const {
+    const int64_t c0 = begin(), c1 = end();
+    return make_piece(shape, seg, shared, block, c0, c1, x, x_end < c1 ? x_end : c1);
+  }
+  __device__ void next(const PagedArgs& a) {
+    const int64_t c1 = end();
+    x = x_end < c1 ? x_end : c1;
+    if (x >= x_end) return;
+    if (++block < seg.blocks) return;
+    block = 0;
+    if (++head < shape.Hkv) return;
+    head = 0;
+    do {
+      seg_start += shape.Hkv * seg.cost;
+      seg = load_segment(a, shape, ++seg_index);  // there is one more with work: x < x_end
+    } while (seg.cost == 0 && seg_index + 1 < segments);
+    enter(a);
+  }
+  __device__ Place place(const PagedArgs& a, const Piece& p, int m, int block_rows) const {
+    const int i = m / shape.group, j = m - i * shape.group;
+    const int64_t t = seg.token0 + i, h = (int64_t)head * shape.group + j;
+    if (p.whole && !a.shared_len)
+      return Place{static_cast<char*>(a.out) + (t * a.Hq + h) * a.D * (a.dtype == PA_BF16 ? 2 : 4), a.lse ? a.lse + h * shape.T + t : nullptr, false};
+    if (p.whole) {
+      const int64_t row = ((shared ? (int64_t)shape.T : 0) + t) * a.Hq + h;
+      return Place{a.rows + row * a.D, a.rows_lse + row, true};
+    }
+    const int64_t row = (2 * (int64_t)position + (x == begin() ? 1 : 0)) * block_rows + (m - block * block_rows);
+    return Place{a.slots + row * a.D, a.slot_lse + row, true};
+  }
+  // What the merge has to know of a block that this share begins and does not end.
+  __device__ PagedCut cut() const {
+    const int64_t c0 = begin(), c1 = end();
+    if (x != c0 || x_end >= c1) return PagedCut{0, 0, 0, 0, 0, 0};
+    return PagedCut{seg.token0, seg.tokens, head, block, position, (int32_t)((c1 - 1) / share)};
+  }
+};
+
+// Finds the workgroup's share; false: it has none.  Every thread of the workgroup calls it.
+template <int THREADS>
+__device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
+  constexpr int WAVES = THREADS / 64;
+  __shared__ int64_t wave_cost[WAVES];
+  __shared__ int64_t found_start;
+  __shared__ int32_t found_segment, first_seq;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  w.shape = a.shape;
+  w.shape.shared = shared_keys(a);
+  const int with = a.shared_len ? 1 : 0;
+  w.segments = a.shape.B + with;
+  if (tid == 0) first_seq = 0x7fffffff;
+  __syncthreads();
+  // Two rounds over the segments where they are more than the threads: the sum of all costs, then the share's segment.
+  int64_t total = 0, start = 0, cost = 0;
+  auto round = [&](int base) {  // start and cost of segment base + tid; total: those before base, and then with this round's
+    const int i = base + tid;
+    cost = 0;
+    if (i < w.segments) {
+      const Segment g = load_segment(a, w.shape, i);
+      cost = w.shape.Hkv * g.cost;
+      if (i >= with && cost > 0) atomicMin(&first_seq, i - with);
+    }
+    int64_t sum = cost;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t up = __shfl_up((long long)sum, d);
+      if (lane >= d) sum += up;
+    }
+    if (lane == 63) wave_cost[wave] = sum;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) {
+      before += v < wave ? wave_cost[v] : 0;
+      all += wave_cost[v];
+    }
+    start = total + before + sum - cost;
+    total += all;
+    __syncthreads();
+  };
+  for (int base = 0; base < w.segments; base += THREADS) {
+    round(base);
+    if (blockIdx.x == 0 && with && base + tid < w.segments) a.seg_start[base + tid] = start;
+  }
+  total = uniform64(total);
+  w.share = share_of(w.shape, total, a.groups);
+  const int32_t active = (int32_t)((total + w.share - 1) / w.share);
+  if (blockIdx.x == 0 && tid == 0) *a.line = PagedLine{w.share, active, w.shape.shared};
+  w.position = position_of(blockIdx.x, active, a.xcds);
+  if (w.position < 0) return false;
+  w.x = w.position * w.share;
+  w.x_end = w.x + w.share < total ? w.x + w.share : total;
+  if (w.segments <= THREADS) {
+    if (start <= w.x && w.x < start + cost) {
+      found_segment = tid;
+      found_start = start;
+    }
+  } else {
+    total = 0;
+    for (int base = 0; base < w.segments; base += THREADS) {
+      round(base);
+      if (start <= w.x && w.x < start + cost) {
+        found_segment = base + tid;
+        found_start = start;
+      }
+    }
+  }
+  __syncthreads();
+  w.seg_index = __builtin_amdgcn_readfirstlane(found_segment);
+  w.seg_start = uniform64(found_start);
+  w.first_seq = __builtin_amdgcn_readfirstlane(first_seq < a.shape.B ? first_seq : a.shape.B - 1);
+  w.seg = load_segment(a, w.shape, w.seg_index);
+  const int64_t off = w.x - w.seg_start;
+  w.head = (int32_t)(off / w.seg.cost);
+  w.block = block_at(w.seg, off - w.head * w.seg.cost);
+  w.enter(a);
+  if (tid == 0) a.cuts[w.position] = PagedCut{0, 0, 0, 0, 0, 0};
+  return true;
+}
+
+}  // namespace pa
