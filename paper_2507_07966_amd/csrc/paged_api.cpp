@@ -186,6 +186,9 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   s.group = plan.group;
   s.block_rows = 16 * a.blocks16;
   s.tile_keys = pa::paged_rows_tile_keys(d.dtype, d.head_dim);
+  s.block_tokens = s.block_rows / s.group;
+  s.inv_groups = 1.0 / a.groups;
+  s.inv_group = 1.0f / (float)s.group;
   s.capacity = d.max_pages_per_seq << plan.page_shift;
   s.start_keys = START_KEYS;
   s.min_share = MIN_SHARE;

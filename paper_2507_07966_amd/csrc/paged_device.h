@@ -82,20 +82,30 @@ struct Walk {
   int32_t position;    // number of the share
   bool shared;         // the segment is that of the shared keys
   int64_t seg_start, x, x_end, share;
+  int32_t token, row_in_group;  // of the block's first row: packed token and index among its group's rows
+  int64_t c0, c1;               // the block's place on the line
 
-  __device__ int64_t begin() const { return seg_start + head * seg.cost + blocks_cost(seg, block); }
-  __device__ int64_t end() const { return begin() + seg.first_cost + block * seg.more_cost; }
   __device__ bool more() const { return x < x_end; }
   __device__ void enter(const PagedArgs& a) {
     shared = a.shared_len && seg_index == 0;
     table_row = shared ? first_seq : seg_index - (a.shared_len ? 1 : 0);
   }
-  __device__ Piece piece() const {
-    const int64_t c0 = begin(), c1 = end();
+  __device__ Piece piece() {
+    c0 = seg_start + head * seg.cost + blocks_cost(seg, block);
+    c1 = c0 + seg.first_cost + (int64_t)block * seg.more_cost;
+    const uint32_t row0 = (uint32_t)(block * shape.block_rows), i = row0 / (uint32_t)shape.group;
+    token = seg.token0 + i;
+    row_in_group = row0 - i * shape.group;
     return make_piece(shape, seg, shared, block, c0, c1, x, x_end < c1 ? x_end : c1);
   }
+  // Rows of the block, and the token (counted from the block's first) and the query head of its row r.
+  __device__ int32_t rows() const {
+    const int32_t left = seg.tokens * shape.group - block * shape.block_rows;
+    return left < shape.block_rows ? left : shape.block_rows;
+  }
+  __device__ int32_t row_token(int32_t r) const { return group_of(shape, row_in_group + r); }
+  __device__ int32_t row_head(int32_t r, int32_t tok) const { return head * shape.group + row_in_group + r - tok * shape.group; }
   __device__ void next(const PagedArgs& a) {
-    const int64_t c1 = end();
     x = x_end < c1 ? x_end : c1;
     if (x >= x_end) return;
     if (++block < seg.blocks) return;
@@ -108,23 +118,22 @@ struct Walk {
     } while (seg.cost == 0 && seg_index + 1 < segments);
     enter(a);
   }
-  __device__ Place place(const PagedArgs& a, const Piece& p, int m, int block_rows) const {
-    const int i = m / shape.group, j = m - i * shape.group;
-    const int64_t t = seg.token0 + i, h = (int64_t)head * shape.group + j;
+  __device__ Place place(const PagedArgs& a, const Piece& p, int r) const {
+    const int32_t tok = row_token(r);
+    const int64_t t = token + tok, h = row_head(r, tok);
     if (p.whole && !a.shared_len)
       return Place{static_cast<char*>(a.out) + (t * a.Hq + h) * a.D * (a.dtype == PA_BF16 ? 2 : 4), a.lse ? a.lse + h * shape.T + t : nullptr, false};
     if (p.whole) {
       const int64_t row = ((shared ? (int64_t)shape.T : 0) + t) * a.Hq + h;
       return Place{a.rows + row * a.D, a.rows_lse + row, true};
     }
-    const int64_t row = (2 * (int64_t)position + (x == begin() ? 1 : 0)) * block_rows + (m - block * block_rows);
+    const int64_t row = (2 * (int64_t)position + (x == c0 ? 1 : 0)) * shape.block_rows + r;
     return Place{a.slots + row * a.D, a.slot_lse + row, true};
   }
-  // What the merge has to know of a block that this share begins and does not end.
-  __device__ PagedCut cut() const {
-    const int64_t c0 = begin(), c1 = end();
-    if (x != c0 || x_end >= c1) return PagedCut{0, 0, 0, 0, 0, 0};
-    return PagedCut{seg.token0, seg.tokens, head, block, position, (int32_t)((c1 - 1) / share)};
+  // Thread 0 notes for the merge a block that this share begins and does not end.
+  __device__ void note_cut(const PagedArgs& a) const {
+    if (threadIdx.x == 0 && x == c0 && x_end < c1)
+      a.cuts[position] = PagedCut{seg.token0, seg.tokens, head, block, position, div_small(c1 - 1, share)};
   }
 };
 
@@ -134,6 +143,7 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   constexpr int WAVES = THREADS / 64;
   __shared__ int64_t wave_cost[WAVES];
   __shared__ int64_t found_start;
+  __shared__ Segment found;
   __shared__ int32_t found_segment, first_seq;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   w.shape = a.shape;
@@ -144,21 +154,22 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   __syncthreads();
   // Two rounds over the segments where they are more than the threads: the sum of all costs, then the share's segment.
   int64_t total = 0, start = 0, cost = 0;
+  Segment g;
+  const int lanes = w.segments < 64 ? w.segments : 64;
   auto round = [&](int base) {  // start and cost of segment base + tid; total: those before base, and then with this round's
     const int i = base + tid;
     cost = 0;
     if (i < w.segments) {
-      const Segment g = load_segment(a, w.shape, i);
+      g = load_segment(a, w.shape, i);
       cost = w.shape.Hkv * g.cost;
       if (i >= with && cost > 0) atomicMin(&first_seq, i - with);
     }
     int64_t sum = cost;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
+    for (int d = 1; d < lanes; d *= 2) {
       const int64_t up = __shfl_up((long long)sum, d);
       if (lane >= d) sum += up;
     }
-    if (lane == 63) wave_cost[wave] = sum;
+    if (lane == lanes - 1) wave_cost[wave] = sum;
     __syncthreads();
     int64_t before = 0, all = 0;
 #pragma unroll
@@ -175,36 +186,37 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
     if (blockIdx.x == 0 && with && base + tid < w.segments) a.seg_start[base + tid] = start;
   }
   total = uniform64(total);
-  w.share = share_of(w.shape, total, a.groups);
-  const int32_t active = (int32_t)((total + w.share - 1) / w.share);
+  w.share = share_of(w.shape, total);
+  const int32_t active = div_small(total + w.share - 1, w.share);
   if (blockIdx.x == 0 && tid == 0) *a.line = PagedLine{w.share, active, w.shape.shared};
   w.position = position_of(blockIdx.x, active, a.xcds);
   if (w.position < 0) return false;
   w.x = w.position * w.share;
   w.x_end = w.x + w.share < total ? w.x + w.share : total;
-  if (w.segments <= THREADS) {
+  if (w.segments > THREADS) total = 0;
+  for (int base = 0; base < w.segments; base += THREADS) {
+    if (w.segments > THREADS) round(base);
     if (start <= w.x && w.x < start + cost) {
-      found_segment = tid;
+      found_segment = base + tid;
       found_start = start;
-    }
-  } else {
-    total = 0;
-    for (int base = 0; base < w.segments; base += THREADS) {
-      round(base);
-      if (start <= w.x && w.x < start + cost) {
-        found_segment = base + tid;
-        found_start = start;
-      }
+      found = g;
     }
   }
   __syncthreads();
   w.seg_index = __builtin_amdgcn_readfirstlane(found_segment);
   w.seg_start = uniform64(found_start);
   w.first_seq = __builtin_amdgcn_readfirstlane(first_seq < a.shape.B ? first_seq : a.shape.B - 1);
-  w.seg = load_segment(a, w.shape, w.seg_index);
+  w.seg.token0 = __builtin_amdgcn_readfirstlane(found.token0);
+  w.seg.tokens = __builtin_amdgcn_readfirstlane(found.tokens);
+  w.seg.key0 = __builtin_amdgcn_readfirstlane(found.key0);
+  w.seg.blocks = __builtin_amdgcn_readfirstlane(found.blocks);
+  w.seg.first_pos = uniform64(found.first_pos);
+  w.seg.first_cost = __builtin_amdgcn_readfirstlane(found.first_cost);
+  w.seg.more_cost = __builtin_amdgcn_readfirstlane(found.more_cost);
+  w.seg.cost = uniform64(found.cost);
   const int64_t off = w.x - w.seg_start;
-  w.head = (int32_t)(off / w.seg.cost);
-  w.block = block_at(w.seg, off - w.head * w.seg.cost);
+  w.head = __builtin_amdgcn_readfirstlane(div_small(off, w.seg.cost));
+  w.block = __builtin_amdgcn_readfirstlane(block_at(w.seg, off - w.head * w.seg.cost));
   w.enter(a);
   if (tid == 0) a.cuts[w.position] = PagedCut{0, 0, 0, 0, 0, 0};
   return true;

@@ -101,9 +101,9 @@ struct CoreBf16 {
     }
   }
   // this lane's channels of query column nq, times f, into its row
-  __device__ void store(float* row, int nq, float f, int g4) const {
+  __device__ void store(f32x4* row, int nq, float f, int g4, int l16) const {
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<f32x4*>(row + 16 * cb + 4 * g4) = O[cb][nq] * f;
+    for (int cb = 0; cb < CB; ++cb) row[(4 * cb + g4) ^ l16] = O[cb][nq] * f;
   }
 };
 
@@ -165,13 +165,13 @@ struct CoreF32 {
             for (int nq = 0; nq < NQ; ++nq)
               O[4 * b + e][nq] = __builtin_amdgcn_mfma_f32_16x16x4f32(V[kb][i][b][e], P[kb][nq][i], O[4 * b + e][nq], 0, 0, 0);
   }
-  __device__ void store(float* row, int nq, float f, int g4) const {
+  __device__ void store(f32x4* row, int nq, float f, int g4, int l16) const {
 #pragma unroll
     for (int b = 0; b < D / 64; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f32x4 x = {O[4 * b][nq][i], O[4 * b + 1][nq][i], O[4 * b + 2][nq][i], O[4 * b + 3][nq][i]};
-        *reinterpret_cast<f32x4*>(row + 64 * b + 16 * g4 + 4 * i) = x * f;
+        row[(16 * b + 4 * g4 + i) ^ l16] = x * f;
       }
   }
 };
@@ -185,7 +185,8 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
   constexpr int LANES_PER_ROW = ROWB / 16, ROWS_PER_LOAD = 1024 / ROWB;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[WAVES * STAGES * 2 * HALF_STAGE];
   __shared__ float wave_max[WAVES][ROWS], wave_sum[WAVES][ROWS];
-  static_assert(WAVES * 16 * (D + 4) * 4 <= (int)sizeof(ring), "the joint fits the ring");
+  constexpr int VECS = D / 4;  // 16-byte pieces of a row of fp32
+  static_assert(WAVES * ROWS * D * 4 <= (int)sizeof(ring), "the joint fits the ring");
 
   Walk walk;
   if (!begin_walk<THREADS>(a, walk)) return;
@@ -208,6 +209,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
   for (; walk.more(); walk.next(a)) {
     const Piece p = walk.piece();
     const Segment& seg = walk.seg;
+    const int block_rows = walk.rows();
     const int32_t* const table = a.page_table + (int64_t)walk.table_row * a.table_width;
     const int first_key = seg.key0 + p.tile0 * shape.tile_keys;
     const int last_key = p.tile1 * shape.tile_keys + seg.key0 < p.key_end ? p.tile1 * shape.tile_keys + seg.key0 : p.key_end;
@@ -224,6 +226,8 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
         pid[kb] = read_const(table, idx < a.table_width ? idx : a.table_width - 1);
       }
     };
+    using B0 = std::integral_constant<int, 0>;
+    using B1 = std::integral_constant<int, 1>;
     int lost[STAGES];  // bit kb: the 16 keys have no page
     auto load = [&](int s, auto buf_c) {
       constexpr int BUF = decltype(buf_c)::value;
@@ -246,33 +250,29 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
         for (int n = 0; n < GROUP_LOADS; ++n) load_chunk_to_lds(vr, dst + HALF_STAGE + kb * 16 * ROWB + n * 1024, loff[n], 0);
       }
     };
-    using B0 = std::integral_constant<int, 0>;
-    using B1 = std::integral_constant<int, 1>;
-    if (stages > 0) look_up(0);
+
+    look_up(0);
 
     int limit[NQ];  // last key that query column nq sees
     int least = 0x7fffffff;
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
-      const int m = p.block * ROWS + nq * 16 + l16;
+      const int r = nq * 16 + l16;
       const T* row = nullptr;
       limit[nq] = 0x7fffffff;
-      if (m < seg.tokens * shape.group) {
-        const int i = m / shape.group, j = m - i * shape.group;
-        row = static_cast<const T*>(a.q) + (int64_t)(seg.token0 + i) * a.q_stride + (int64_t)(walk.head * shape.group + j) * D;
-        if (!walk.shared) limit[nq] = (int)clamp64(seg.first_pos + i, -1, shape.capacity);
+      if (r < block_rows) {
+        const int tok = walk.row_token(r);
+        row = static_cast<const T*>(a.q) + (int64_t)(walk.token + tok) * a.q_stride + walk.row_head(r, tok) * D;
+        if (!walk.shared) limit[nq] = (int)clamp64(seg.first_pos + (walk.token - seg.token0) + tok, -1, shape.capacity);
       }
       core.load_q(nq, row, g4);
       least = limit[nq] < least ? limit[nq] : least;
     }
-    if (stages > 0) {
-      load(0, B0{});
-      if (stages > 1) {
-        look_up(1);
-        load(1, B1{});
-        if (stages > 2) look_up(2);
-      }
-    }
+    // Also where this wavefront has fewer stages (the loads are then empty): the compiler counts what is under way.
+    load(0, B0{});
+    look_up(1);
+    load(1, B1{});
+    if (stages > 2) look_up(2);
 #pragma unroll
     for (int x = 1; x < 16; x *= 2) {
       const int other = __shfl_xor(least, x);
@@ -359,7 +359,8 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       if (s + 1 < stages) step(s + 1, B1{});
     }
 
-    // ---- join the wavefronts: reference maxima first, then the outputs, 16 rows at a time through LDS
+    // ---- join the wavefronts: reference maxima, then the outputs, all of the block's rows at once through LDS (16-byte chunk c of row r
+    //      at chunk c ^ (r & 15): rows written by 16 lanes at one chunk fall on all banks)
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
       const float l = quad_sum(sum[nq]);
@@ -369,48 +370,35 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       }
     }
     __syncthreads();  // all loads are done and all reads of the ring are over
-    float* const joint = reinterpret_cast<float*>(ring);
-    constexpr int STRIDE = D + 4;
+    f32x4* const joint = reinterpret_cast<f32x4*>(ring);
+    auto factor = [&](float from, float to) { return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from - to) * c_log2); };
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
+      const int r = nq * 16 + l16;
       float m = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) m = fmaxf(m, wave_max[w][nq * 16 + l16]);
-      const float f = top[nq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top[nq] - m) * c_log2);
-      core.store(joint + (wave * 16 + l16) * STRIDE, nq, f, g4);
-      __syncthreads();
-      {
-        constexpr int PER = D / 16;  // channels of a thread
-        const int r = tid >> 4, ch = (tid & 15) * 4;
-        float mr = -INFINITY, lr = 0.f;
+      for (int w = 0; w < WAVES; ++w) m = fmaxf(m, wave_max[w][r]);
+      if (r < block_rows) core.store(joint + (wave * ROWS + r) * VECS, nq, factor(top[nq], m), g4, l16);
+    }
+    __syncthreads();
+    for (int idx = tid; idx < block_rows * VECS; idx += THREADS) {
+      const int r = idx / VECS, v = idx % VECS;
+      float m = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) mr = fmaxf(mr, wave_max[w][nq * 16 + r]);
+      for (int w = 0; w < WAVES; ++w) m = fmaxf(m, wave_max[w][r]);
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-          const float mw = wave_max[w][nq * 16 + r];
-          lr += wave_sum[w][nq * 16 + r] * (mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - mr) * c_log2));
-        }
-        const float inv = lr == 0.f ? 0.f : 1.f / lr;  // 0: no key is seen
-        const float lse = mr * a.scale + logf(lr);
-        const int m_row = p.block * ROWS + nq * 16 + r;
-        if (m_row < seg.tokens * shape.group) {
-          const Place dst = walk.place(a, p, m_row, ROWS);
-#pragma unroll
-          for (int x = 0; x < PER / 4; ++x) {
-            f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) v += *reinterpret_cast<const f32x4*>(joint + (w * 16 + r) * STRIDE + 64 * x + ch);
-            write_row<T>(dst, 64 * x + ch, v * inv);
-          }
-          if (ch == 0 && dst.lse) *dst.lse = lse;
-        }
+      for (int w = 0; w < WAVES; ++w) {
+        l += wave_sum[w][r] * factor(wave_max[w][r], m);
+        o += joint[(w * ROWS + r) * VECS + (v ^ (r & 15))];
       }
-      __syncthreads();  // the joint is read before the next 16 rows or the next block's loads come
+      const float inv = l == 0.f ? 0.f : 1.f / l;  // 0: no key is seen
+      const Place dst = walk.place(a, p, r);
+      write_row<T>(dst, 4 * v, o * inv);
+      if (v == 0 && dst.lse) *dst.lse = m * a.scale + __logf(l);
     }
-    if (tid == 0) {
-      const PagedCut cut = walk.cut();
-      if (cut.tokens) a.cuts[walk.position] = cut;
-    }
+    walk.note_cut(a);
+    __syncthreads();  // the joint is read before the next block's loads come
   }
 }
 
