@@ -52,7 +52,7 @@ struct PagedArgs {
   float scale;
   PagedShape shape;        // `shared` is read on the device
   int32_t groups, xcds;    // workgroups, and over how many XCDs they are laid out
-  int32_t blocks16;        // 16-row blocks of an item
+  int32_t blocks16;        // few rows: 16-row blocks of a block
   // workspace
   PagedLine* line;
   int64_t* seg_start;      // [B + 2] cost at which segment i begins (with shared keys only: segment 0 is theirs)
@@ -64,6 +64,8 @@ struct PagedArgs {
 };
 int launch_paged_rows(const PagedArgs& a, void* stream);   // calls of few rows a sequence, and fp32
 int paged_rows_tile_keys(int32_t dtype, int32_t D);        // keys that its wavefronts share out in a step
+constexpr int PAGED_CHUNK_ROWS = 256, PAGED_CHUNK_KEYS = 64;
+int launch_paged_chunk(const PagedArgs& a, void* stream);  // bf16 calls of many rows a sequence
 int launch_paged_merge(const PagedArgs& a, void* stream);
 
 }  // namespace pa

@@ -152,6 +152,10 @@ constexpr int64_t FEW_ROWS = 64;
 
 // A block's start and end cost about as much as this many keys, and a share of fewer keys is not worth a workgroup and a merge.
 constexpr int32_t START_KEYS = 64, MIN_SHARE = 256;
+constexpr int32_t CHUNK_START_KEYS = 128, CHUNK_MIN_SHARE = 512;
+
+// bf16 calls of more rows a sequence than a block of few rows holds run in blocks of PAGED_CHUNK_ROWS
+bool is_chunk(int64_t rows, int64_t num_seqs, int32_t dtype) { return dtype == PA_BF16 && rows > FEW_ROWS * num_seqs; }
 
 pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
                       const int32_t* page_table, const int32_t* seq_lens, const int32_t* cu_new, int32_t num_seqs, int32_t num_tokens,
@@ -184,14 +188,16 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   s.T = num_tokens;
   s.Hkv = d.num_kv_heads;
   s.group = plan.group;
-  s.block_rows = 16 * a.blocks16;
-  s.tile_keys = pa::paged_rows_tile_keys(d.dtype, d.head_dim);
+  const bool chunk = is_chunk(rows, num_seqs, d.dtype);
+  s.block_rows = chunk ? pa::PAGED_CHUNK_ROWS : 16 * a.blocks16;
+  s.tile_keys = chunk ? pa::PAGED_CHUNK_KEYS : pa::paged_rows_tile_keys(d.dtype, d.head_dim);
+  s.causal_cuts = chunk;
   s.block_tokens = s.block_rows / s.group;
   s.inv_groups = 1.0 / a.groups;
   s.inv_group = 1.0f / (float)s.group;
   s.capacity = d.max_pages_per_seq << plan.page_shift;
-  s.start_keys = START_KEYS;
-  s.min_share = MIN_SHARE;
+  s.start_keys = chunk ? CHUNK_START_KEYS : START_KEYS;
+  s.min_share = chunk ? CHUNK_MIN_SHARE : MIN_SHARE;
   a.line = reinterpret_cast<pa::PagedLine*>(ws);
   a.seg_start = reinterpret_cast<int64_t*>(ws + plan.off_seg_start);
   a.cuts = reinterpret_cast<pa::PagedCut*>(ws + plan.off_cuts);
@@ -252,7 +258,7 @@ int paged_attn_plan(const paged_attn_desc_t* desc, paged_attn_plan_t** plan_out,
     p->num_xcd = n == 256 ? 8 : 1;  // the layout that shares are spread over XCDs for
   }
   // What the shares leave of blocks that they cut, and, where shared keys are a segment of their own, partials of all rows.
-  const int64_t block_rows = 64, slots = 2 * (int64_t)p->num_cu * block_rows;
+  const int64_t block_rows = is_chunk(d.max_tokens * p->group, 1, d.dtype) ? pa::PAGED_CHUNK_ROWS : 64, slots = 2 * (int64_t)p->num_cu * block_rows;
   const int64_t few = FEW_ROWS * d.max_seqs / p->group, tokens = few < d.max_tokens ? few : d.max_tokens;
   size_t at = 256;
   auto take = [&](size_t bytes) {
@@ -309,7 +315,8 @@ int paged_attn_forward(const paged_attn_plan_t* plan, const void* q, int64_t q_s
   if ((st = check_device(d)) != PA_OK) return st;
   const pa::PagedArgs a = arrange(*plan, q, q_stride, k_cache, v_cache, page_table, seq_lens, cu_new, num_seqs, (int32_t)num_tokens,
                                   shared_len, out, lse_out, static_cast<char*>(workspace));
-  if (pa::launch_paged_rows(a, hip_stream) != 0) return PA_ERR_HIP;
+  const bool chunk = is_chunk(num_tokens * plan->group, num_seqs, d.dtype);
+  if ((chunk ? pa::launch_paged_chunk(a, hip_stream) : pa::launch_paged_rows(a, hip_stream)) != 0) return PA_ERR_HIP;
   return pa::launch_paged_merge(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
 }
 

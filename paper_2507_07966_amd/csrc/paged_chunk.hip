@@ -1,0 +1,344 @@
+// Attention of new tokens over their pages for chunks (bf16): blocks of 256 stacked rows.
+//
+// Bound: bf16 MFMA.  A block is 256 rows m = i * group + (h % group) of one kv head and sequence, 32 a wavefront, two wavefronts a SIMD;
+// tiles of 64 keys go to LDS once for all of them, two of K and two of V, one barrier a tile.  Products, operand order and the
+// interleave of one tile's softmax with the product before are those of the prefill kernels (v_mfma_f32_16x16x32_bf16 on transposed
+// scores); what differs:
+//   - Keys come from pages.  A wavefront loads 8 rows of a tile; they lie in one page (page sizes are multiples of 16), whose
+//     number is read into scalar registers one tile ahead, and the buffer descriptor is made for them: 64-bit address, range up to the
+//     last key, so that nothing past it is read and LDS holds zeros there.  Rows without a page become NaN keys.
+//   - V is read transposed from row-major tiles (ds_read_b64_tr_b16): a paged cache has no images of its values.
+//   - The reference of the softmax is the maximum of a row's first tile, with no search afterwards; a tile's sum tells when some
+//     probability left the safe range.  Then the block is done again with its true maxima, which a pass over the
+//     scores alone finds first: one loop serves both, and no code that rescales accumulators takes registers from it.
+//   - A workgroup takes a share of the line of paged_sched.h: whole blocks, and parts of the two that its ends cut.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "common.h"
+#include "mfma_tiles.h"
+#include "paged.h"
+#include "paged_device.h"
+
+namespace pa {
+namespace {
+
+using namespace mt;
+
+constexpr int NQ = 2, WAVES = 8, THREADS = WAVES * 64, ROWS_PER_WAVE = 16 * NQ, ROWS = WAVES * ROWS_PER_WAVE;
+static_assert(ROWS == PAGED_CHUNK_ROWS && TILE == PAGED_CHUNK_KEYS, "the schedule's blocks and tiles");
+constexpr float SAFE_SUM = 65536.0f;  // a lane's sum of a tile's probabilities below this keeps fp32 and bf16 far from overflow
+constexpr int RING = 4;               // LDS operand reads ahead of the MFMAs that use them
+
+template <int D>
+__global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs a) {
+  constexpr int ROWB = 2 * D, TILE_BYTES = TILE * ROWB, KS = D / 32, CB = D / 16;
+  constexpr int LOADS = TILE_BYTES / 1024 / WAVES;  // 1 KiB loads of a wavefront, of K and of V
+  constexpr int LANES_PER_ROW = ROWB / 16, ROWS_PER_LOAD = 1024 / ROWB;
+  constexpr int WAVE_KEYS = TILE / WAVES;           // rows of a tile that a wavefront loads
+  constexpr int VBUF = 2 * TILE_BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_BYTES];
+  __shared__ int32_t gave_up[WAVES];
+
+  Walk walk;
+  if (!begin_walk<THREADS>(a, walk)) return;
+  const PagedShape& shape = walk.shape;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int page_mask = (1 << a.page_shift) - 1;
+  const float c_log2 = a.scale * 1.4426950408889634f;
+
+  int koff[KS], vtr[CB];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) koff[ks] = l16 * ROWB + (((4 * ks + g4) ^ swizzle_term(l16, ROWB)) << 4);
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int r = 4 * g4 + (l16 >> 2);
+    vtr[cb] = r * ROWB + (((2 * cb + ((l16 & 3) >> 1)) ^ swizzle_term_tr(r, ROWB)) << 4) + (l16 & 1) * 8;
+  }
+  unsigned kload[LOADS], vload[LOADS];  // byte offset of this lane's 16 bytes in the wavefront's rows of the cache
+#pragma unroll
+  for (int n = 0; n < LOADS; ++n) {
+    const int in = n * ROWS_PER_LOAD + lane / LANES_PER_ROW, row = wave * WAVE_KEYS + in;
+    kload[n] = (unsigned)(in * ROWB + (((lane % LANES_PER_ROW) ^ swizzle_term(row, ROWB)) << 4));
+    vload[n] = (unsigned)(in * ROWB + (((lane % LANES_PER_ROW) ^ swizzle_term_tr(row, ROWB)) << 4));
+  }
+
+  for (; walk.more(); walk.next(a)) {
+    const Piece p = walk.piece();
+    const Segment& seg = walk.seg;
+    const int block_rows = walk.rows();
+    const int32_t* const table = a.page_table + (int64_t)walk.table_row * a.table_width;
+    const int first_key = seg.key0 + p.tile0 * TILE, tiles = p.tile1 - p.tile0;
+
+    // ---- this lane's two query columns
+    bf16x8 Q[NQ][KS];
+    int limit[NQ];  // last key that column nq sees
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      const int r = wave * ROWS_PER_WAVE + nq * 16 + l16;
+      const __bf16* row = nullptr;
+      limit[nq] = 0x7fffffff;
+      if (r < block_rows) {
+        const int tok = walk.row_token(r);
+        row = static_cast<const __bf16*>(a.q) + (int64_t)(walk.token + tok) * a.q_stride + walk.row_head(r, tok) * D + 8 * g4;
+        limit[nq] = (int)clamp64(seg.first_pos + (walk.token - seg.token0) + tok, -1, shape.capacity);
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) Q[nq][ks] = row ? *reinterpret_cast<const bf16x8*>(row + 32 * ks) : bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    // keys up to this one are seen by every row of the wavefront (positions do not fall from row to row)
+    const int first_limit = __builtin_amdgcn_readfirstlane(limit[0]);
+
+    // The pages of a wavefront's rows of tile t: K's is looked up one tile before it is used, and V's is the same, one step later.
+    auto look_up = [&](int t) {
+      const int idx = (first_key + t * TILE + wave * WAVE_KEYS) >> a.page_shift;
+      const int page = read_const(table, idx < a.table_width ? idx : a.table_width - 1);
+      return idx < a.table_width && page >= 0 && page < a.num_pages ? page : -1;
+    };
+    auto base_of = [&](int t, int page) -> int64_t {
+      const int key = first_key + t * TILE + wave * WAVE_KEYS;
+      return page < 0 ? 0 : ((((int64_t)page * shape.Hkv + walk.head) << a.page_shift) + (key & page_mask)) * ROWB;
+    };
+    auto bytes_of = [&](int t, int page) {
+      const int left = p.key_end - (first_key + t * TILE + wave * WAVE_KEYS);
+      return page < 0 || left <= 0 ? 0 : (left < WAVE_KEYS ? left : WAVE_KEYS) * ROWB;
+    };
+    auto issue_k = [&](int t, int page, auto buf_c) {
+      unsigned char* const dst = smem + decltype(buf_c)::value * TILE_BYTES + wave * LOADS * 1024;
+      if (page < 0 && first_key + t * TILE + wave * WAVE_KEYS < p.key_end) {
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) *reinterpret_cast<i32x4*>(dst + n * 1024 + lane * 16) = i32x4{0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0};
+        return;
+      }
+      const rsrc_t rs = make_rsrc(static_cast<const char*>(a.k_cache) + base_of(t, page), bytes_of(t, page));
+#pragma unroll
+      for (int n = 0; n < LOADS; ++n) load_chunk_to_lds(rs, dst + n * 1024, kload[n], 0);
+    };
+    auto issue_v = [&](int t, int page, auto buf_c) {
+      unsigned char* const dst = smem + VBUF + decltype(buf_c)::value * TILE_BYTES + wave * LOADS * 1024;
+      const rsrc_t rs = make_rsrc(static_cast<const char*>(a.v_cache) + base_of(t, page), bytes_of(t, page));
+#pragma unroll
+      for (int n = 0; n < LOADS; ++n) load_chunk_to_lds(rs, dst + n * 1024, vload[n], 0);
+    };
+
+    f32x4 O[CB][NQ];    // O^T: register i of block cb is channel 16 cb + 4 g4 + i of column nq
+    f32x4 S[4][NQ];     // scores of the tile being soft-maxed: register i of block kb is key 16 kb + 4 g4 + i
+    bf16x8 Pb[2][NQ];   // probabilities of the tile before, as the operand of its product with V
+    float mref[NQ], lsum[NQ];
+    bool bad = false;
+
+    auto scores = [&](const unsigned char* kbuf, auto&& mid) {
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) S[kb][nq] = f32x4{0.f, 0.f, 0.f, 0.f};
+      auto operand = [&](int t) { return lds_operand(kbuf + (t % 4) * 16 * ROWB + koff[t / 4]); };
+      constexpr int OPS = 4 * KS;
+      bf16x8 ka[RING];
+#pragma unroll
+      for (int t = 0; t < RING; ++t) ka[t] = operand(t);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int t = 0; t < OPS; ++t) {
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+          S[t % 4][nq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[t % RING], Q[nq][t / 4], S[t % 4][nq], 0, 0, 0);
+        if (t + RING < OPS) ka[t % RING] = operand(t + RING);
+        mid(t);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+    };
+    auto mask = [&](int t) {
+      const int key0 = first_key + t * TILE;
+      if (key0 + TILE - 1 > first_limit) {
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (key0 + 16 * kb + 4 * g4 + i > limit[nq]) S[kb][nq][i] = -INFINITY;
+      }
+    };
+    auto row_max = [&](int nq) {
+      float m = S[0][nq][0];
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, S[kb][nq][i]);
+      return quad_max(m);
+    };
+    auto reference = [&](int nq) { return mref[nq] == -INFINITY ? 0.f : mref[nq] * c_log2; };  // -inf: no key is seen
+    // probabilities of block j = NQ kb + nq, rounded to bf16 for the product with V; their sum is taken before rounding
+    auto slice = [&](int j, const float (&mc)[NQ], bf16x8 (&Pn)[2][NQ], float (&lacc)[NQ]) {
+      const int kb = j / NQ, nq = j % NQ;
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const f32x2 pr = {__builtin_amdgcn_exp2f(__builtin_fmaf(S[kb][nq][e], c_log2, -mc[nq])),
+                          __builtin_amdgcn_exp2f(__builtin_fmaf(S[kb][nq][e + 1], c_log2, -mc[nq]))};
+        const bf16x2 pk = __builtin_convertvector(pr, bf16x2);
+        lacc[nq] += pr[0] + pr[1];
+        Pn[kb >> 1][nq][(kb & 1) * 4 + e] = pk[0];
+        Pn[kb >> 1][nq][(kb & 1) * 4 + e + 1] = pk[1];
+      }
+    };
+    auto accept = [&](const bf16x8 (&Pn)[2][NQ], const float (&lacc)[NQ]) {
+      bool unsafe = false;
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        unsafe = unsafe || !(lacc[nq] <= SAFE_SUM);  // also NaN
+        lsum[nq] += lacc[nq];
+#pragma unroll
+        for (int c32 = 0; c32 < 2; ++c32) Pb[c32][nq] = Pn[c32][nq];
+      }
+      bad = bad || __any(unsafe);
+    };
+    // O^T += V^T P^T for the tile in Pb, interleaved with the softmax of the tile in S
+    auto product = [&](const unsigned char* vbuf, auto overlap_c, bf16x8 (&Pn)[2][NQ], float (&lacc)[NQ]) {
+      constexpr int OPS = 2 * CB;
+      float mc[NQ];
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) mc[nq] = reference(nq);
+      auto operand = [&](int t) {
+        const unsigned char* v = vbuf + (t / CB) * 32 * ROWB + vtr[t % CB];
+        return lds_operand_tr(v, v + 16 * ROWB);
+      };
+      bf16x8 va[RING];
+#pragma unroll
+      for (int t = 0; t < RING; ++t) va[t] = operand(t);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int t = 0; t < OPS; ++t) {
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+          O[t % CB][nq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[t % RING], Pb[t / CB][nq], O[t % CB][nq], 0, 0, 0);
+        if (t + RING < OPS) va[t % RING] = operand(t + RING);
+        if (decltype(overlap_c)::value) {
+#pragma unroll
+          for (int j = t * (4 * NQ) / OPS; j < (t + 1) * (4 * NQ) / OPS; ++j) slice(j, mc, Pn, lacc);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    using B0 = std::integral_constant<int, 0>;
+    using B1 = std::integral_constant<int, 1>;
+    // Once; and, where some row's probabilities left the safe range, once more with the true maxima.
+    for (int again = 0; tiles > 0; ++again) {
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        mref[nq] = -INFINITY;
+        lsum[nq] = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) O[cb][nq] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      bad = false;
+      if (again) {
+        for (int t = 0; t < tiles; ++t) {
+          issue_k(t, look_up(t), B0{});
+          wait_loads<0>();
+          __syncthreads();
+          scores(smem, [](int) {});
+          mask(t);
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) mref[nq] = fmaxf(mref[nq], row_max(nq));
+          __syncthreads();
+        }
+      }
+      int page = look_up(0), page1 = look_up(1);  // of the tile whose V comes next, and of the tile whose K does
+      issue_k(0, page, B0{});
+      issue_v(0, page, B0{});
+      if (tiles > 1) issue_k(1, page1, B1{});
+      wait_loads<0>();
+      __syncthreads();
+      scores(smem, [](int) {});
+      mask(0);
+      {
+        bf16x8 Pn[2][NQ];
+        float lacc[NQ], mc[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+          if (!again) {
+            mref[nq] = row_max(nq);
+            bad = bad || __any(mref[nq] == -INFINITY);  // a row without a key in its first tile has no reference yet
+          }
+          mc[nq] = reference(nq);
+          lacc[nq] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4 * NQ; ++j) slice(j, mc, Pn, lacc);
+        accept(Pn, lacc);
+      }
+      __syncthreads();
+      auto step = [&](int t, auto buf_c) {
+        constexpr int BUF = decltype(buf_c)::value;
+        const int page2 = look_up(t + 1);
+        scores(smem + BUF * TILE_BYTES, [&](int o) {
+          if (o == 1 && t + 1 < tiles) issue_k(t + 1, page2, std::integral_constant<int, BUF ^ 1>{});
+          if (o == 2 * KS + 1) issue_v(t, page1, buf_c);
+        });
+        page1 = page2;
+        mask(t);
+        bf16x8 Pn[2][NQ];
+        float lacc[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) lacc[nq] = 0.f;
+        product(smem + VBUF + (BUF ^ 1) * TILE_BYTES, std::true_type{}, Pn, lacc);
+        accept(Pn, lacc);
+        wait_loads<0>();
+        __syncthreads();
+      };
+      int t = 1;
+      for (; t + 1 < tiles; t += 2) {
+        step(t, B1{});
+        step(t + 1, B0{});
+      }
+      if (t < tiles) step(t, B1{});
+      {
+        bf16x8 Pn[2][NQ];
+        float lacc[NQ];
+        product(smem + VBUF + ((tiles - 1) & 1) * TILE_BYTES, std::false_type{}, Pn, lacc);
+      }
+      if (again) break;
+      if (lane == 0) gave_up[wave] = bad ? 1 : 0;
+      __syncthreads();
+      int any = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) any |= gave_up[w];
+      if (__builtin_amdgcn_readfirstlane(any) == 0) break;
+      __syncthreads();
+    }
+
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      const int r = wave * ROWS_PER_WAVE + nq * 16 + l16;
+      const float l = tiles > 0 ? quad_sum(lsum[nq]) : 0.f;
+      const float inv = l == 0.f ? 0.f : 1.f / l;  // 0: no key is seen
+      if (r < block_rows) {
+        const Place dst = walk.place(a, p, r);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) write_row<__bf16>(dst, 16 * cb + 4 * g4, tiles > 0 ? O[cb][nq] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
+        if (g4 == 0 && dst.lse) *dst.lse = tiles > 0 ? mref[nq] * a.scale + __logf(l) : -INFINITY;
+      }
+    }
+    walk.note_cut(a);
+    __syncthreads();  // all reads of the tiles are over before the next block's loads come
+  }
+}
+
+}  // namespace
+
+int launch_paged_chunk(const PagedArgs& a, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a.D == 128) paged_chunk_kernel<128><<<a.groups, THREADS, 0, s>>>(a);
+  else paged_chunk_kernel<64><<<a.groups, THREADS, 0, s>>>(a);
+  return (int)hipGetLastError();
+}
+
+}  // namespace pa

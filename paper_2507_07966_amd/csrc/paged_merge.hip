@@ -3,7 +3,8 @@
 // Without shared keys, workgroup (share, y) looks whether its share begins a block that it does not end, and merges rows of that block: the
 // last piece that share left and what the shares after it left of the same block.  With shared keys every row has
 // pieces of its own keys and of the shared ones: a workgroup per row finds both from the line.  Bound: latency; a row's D / 4 vectors are
-// spread over lanes and its pieces over groups of lanes, whose sums are joined through LDS.
+// spread over lanes and its pieces over groups of lanes, whose sums are joined through LDS.  Blocks of many rows have few pieces: there a
+// workgroup takes several rows at once, a lane all pieces of its vector.
 #include <hip/hip_runtime.h>
 
 #include "paged.h"
@@ -24,18 +25,20 @@ struct Pieces {
   int32_t first_share, row;  // further pieces: slot 2 (first_share + i), row `row` of it
 };
 
-template <typename T, int D>
+template <int D, int PARTS_>
 struct Joint {
-  static constexpr int VECS = D / 4, PARTS = THREADS / VECS;  // lanes of a row, pieces worked on at once
+  static constexpr int VECS = D / 4, PARTS = PARTS_;  // lanes of a row, pieces worked on at once
+  static constexpr int ROWS = THREADS / VECS / PARTS;  // rows of a workgroup
+  static_assert(PARTS == 1 || ROWS == 1, "either several pieces at once or several rows");
   f32x4 acc[PARTS][VECS];
   float top[PARTS], sum[PARTS];
 };
 
-// Every thread of the workgroup calls it; `parts` lists of pieces make up the row.
-template <typename T, int D>
-__device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], int lists, int64_t t, int64_t h, Joint<T, D>& joint) {
-  using J = Joint<T, D>;
-  const int vec = threadIdx.x % J::VECS, part = threadIdx.x / J::VECS;
+// The row is made up of one or two lists of pieces.  With several pieces at once every thread of the workgroup calls it, for one row.
+template <typename T, int D, int PARTS>
+__device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], int lists, int64_t t, int64_t h, Joint<D, PARTS>& joint) {
+  using J = Joint<D, PARTS>;
+  const int vec = threadIdx.x % J::VECS, part = PARTS == 1 ? 0 : threadIdx.x / J::VECS;
   const int block_rows = a.shape.block_rows;
   const int n0 = list[0].count, n = n0 + (lists > 1 ? list[1].count : 0);
   auto at = [&](int i, const float*& o, const float*& l) {
@@ -78,51 +81,53 @@ __device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], in
       acc += w * o[e];
     }
   }
-  joint.acc[part][vec] = acc;
-  if (vec == 0) {
-    joint.top[part] = top;
-    joint.sum[part] = sum;
-  }
-  __syncthreads();
-  if (part == 0) {
+  if constexpr (PARTS > 1) {
+    joint.acc[part][vec] = acc;
+    if (vec == 0) {
+      joint.top[part] = top;
+      joint.sum[part] = sum;
+    }
+    __syncthreads();
+    if (part) return;
     top = -INFINITY;
     sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int p = 0; p < J::PARTS; ++p) top = fmaxf(top, joint.top[p]);
+    for (int p = 0; p < PARTS; ++p) top = fmaxf(top, joint.top[p]);
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int p = 0; p < J::PARTS; ++p) {
+    for (int p = 0; p < PARTS; ++p) {
       const float w = expf(joint.top[p] - ref);
       sum += w * joint.sum[p];
       acc += w * joint.acc[p][vec];
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // 0: no piece has a key that the row sees
-    write_row<T>(Place{static_cast<T*>(a.out) + (t * a.Hq + h) * D, nullptr, false}, 4 * vec, acc * inv);
-    if (vec == 0 && a.lse) a.lse[h * a.shape.T + t] = ref + logf(sum);
   }
-  __syncthreads();
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // 0: no piece has a key that the row sees
+  write_row<T>(Place{static_cast<T*>(a.out) + (t * a.Hq + h) * D, nullptr, false}, 4 * vec, acc * inv);
+  if (vec == 0 && a.lse) a.lse[h * a.shape.T + t] = (top == -INFINITY ? 0.f : top) + logf(sum);
 }
 
-template <typename T, int D>
+// blockIdx.y: which rows of the block
+template <typename T, int D, int PARTS>
 __global__ __launch_bounds__(THREADS) void merge_cuts_kernel(const PagedArgs a) {
   const int position = blockIdx.x;
   if (position >= a.line->active) return;
   const PagedCut c = a.cuts[position];
   if (c.tokens == 0) return;
-  __shared__ Joint<T, D> joint;
-  const int block_rows = a.shape.block_rows, rows = c.tokens * a.shape.group - c.block * block_rows;
-  const int last = rows < block_rows ? rows : block_rows;
-  for (int r = blockIdx.y; r < last; r += gridDim.y) {
-    const int m = c.block * block_rows + r, i = m / a.shape.group, j = m - i * a.shape.group;
-    const Pieces list[2] = {{c.last - c.first + 1, (2 * (int64_t)c.first + 1) * block_rows + r, false, c.first, r}, {}};
-    merge_row<T, D>(a, list, 1, c.token0 + i, (int64_t)c.head * a.shape.group + j, joint);
-  }
+  using J = Joint<D, PARTS>;
+  __shared__ J joint;
+  const int r = blockIdx.y * J::ROWS + (PARTS == 1 ? threadIdx.x / J::VECS : 0);
+  const int m = c.block * a.shape.block_rows + r;
+  if (m >= c.tokens * a.shape.group) return;
+  const int i = (uint32_t)m / (uint32_t)a.shape.group, j = m - i * a.shape.group;
+  const Pieces list[2] = {{c.last - c.first + 1, (2 * (int64_t)c.first + 1) * a.shape.block_rows + r, false, c.first, r}, {}};
+  merge_row<T, D, PARTS>(a, list, 1, c.token0 + i, (int64_t)c.head * a.shape.group + j, joint);
 }
 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) {
-  __shared__ Joint<T, D> joint;
+  constexpr int PARTS = THREADS / (D / 4);
+  __shared__ Joint<D, PARTS> joint;
   __shared__ int seq;
   const int64_t t = blockIdx.x;
   const int64_t h = blockIdx.y;
@@ -147,7 +152,7 @@ __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) 
   };
   const Segment own = load_segment(a, s, b + 1), all = load_segment(a, s, 0);
   const Pieces list[2] = {pieces(own, a.seg_start[b + 1], false), t < all.tokens ? pieces(all, a.seg_start[0], true) : Pieces{}};
-  merge_row<T, D>(a, list, 2, t, h, joint);
+  merge_row<T, D, PARTS>(a, list, 2, t, h, joint);
 }
 
 template <typename T, int D>
@@ -155,8 +160,11 @@ int launch(const PagedArgs& a, hipStream_t s) {
   if (a.shared_len) {
     merge_rows_kernel<T, D><<<dim3((unsigned)a.shape.T, (unsigned)a.Hq), THREADS, 0, s>>>(a);
   } else {
-    const int rows = a.shape.block_rows < 64 ? a.shape.block_rows : 64;
-    merge_cuts_kernel<T, D><<<dim3((unsigned)a.groups, (unsigned)rows), THREADS, 0, s>>>(a);
+    const int64_t rows = (int64_t)a.shape.T * a.shape.group;  // of a kv head, in all
+    const int most = rows < a.shape.block_rows ? (int)rows : a.shape.block_rows;
+    constexpr int LANES = THREADS / (D / 4);
+    if (a.shape.block_rows > 64) merge_cuts_kernel<T, D, 1><<<dim3((unsigned)a.groups, (unsigned)((most + LANES - 1) / LANES)), THREADS, 0, s>>>(a);
+    else merge_cuts_kernel<T, D, LANES><<<dim3((unsigned)a.groups, (unsigned)most), THREADS, 0, s>>>(a);
   }
   return (int)hipGetLastError();
 }
