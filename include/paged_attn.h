@@ -129,6 +129,19 @@ int paged_attn_forward(const paged_attn_plan_t* plan, const void* q, int64_t q_s
                        int32_t num_seqs, int64_t num_tokens, const int32_t* shared_len, void* out, float* lse_out,
                        void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- introspection of the schedule (host only; used by tests) ----
+ *
+ * The pieces of work that paged_attn_forward's workgroups take for these lengths (HOST arrays, as they would be on the device;
+ * shared_len < 0: not given).  pieces_out [max_pieces][8] receives, in the order of the shares,
+ *     {share, sequence (-1: the shared keys, with the rows of all sequences), kv head, first stacked row of the block (m = i * (Hq / Hkv) +
+ *      h % (Hq / Hkv) over the sequence's new tokens), rows, first key, end of the keys, 1 if the piece is its whole block}.
+ * Returns their number (also where it exceeds max_pieces), or minus a status code. */
+int64_t paged_attn_schedule(const paged_attn_plan_t* plan, const int32_t* seq_lens, const int32_t* cu_new, int32_t num_seqs,
+                            int64_t num_tokens, int32_t shared_len, int32_t* pieces_out, int64_t max_pieces);
+/* The workgroups of such a call, the rows of a block and the keys of a tile. */
+int paged_attn_schedule_shape(const paged_attn_plan_t* plan, int32_t num_seqs, int64_t num_tokens, int32_t with_shared,
+                              int32_t* groups, int32_t* block_rows, int32_t* tile_keys);
+
 #ifdef __cplusplus
 }
 #endif

@@ -320,4 +320,64 @@ int paged_attn_forward(const paged_attn_plan_t* plan, const void* q, int64_t q_s
   return pa::launch_paged_merge(a, hip_stream) == 0 ? PA_OK : PA_ERR_HIP;
 }
 
+int paged_attn_schedule_shape(const paged_attn_plan_t* plan, int32_t num_seqs, int64_t num_tokens, int32_t with_shared, int32_t* groups,
+                              int32_t* block_rows, int32_t* tile_keys) {
+  if (!plan || !groups || !block_rows || !tile_keys) return PA_ERR_NULL;
+  if (num_seqs < 1 || num_seqs > plan->desc.max_seqs || num_tokens < 1 || num_tokens > plan->desc.max_tokens) return PA_ERR_SHAPE;
+  const int32_t given = 0;
+  const pa::PagedArgs a = arrange(*plan, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr, num_seqs, (int32_t)num_tokens,
+                                  with_shared ? &given : nullptr, nullptr, nullptr, nullptr);
+  *groups = a.groups;
+  *block_rows = a.shape.block_rows;
+  *tile_keys = a.shape.tile_keys;
+  return PA_OK;
+}
+
+int64_t paged_attn_schedule(const paged_attn_plan_t* plan, const int32_t* seq_lens, const int32_t* cu_new, int32_t num_seqs,
+                            int64_t num_tokens, int32_t shared_len, int32_t* pieces_out, int64_t max_pieces) {
+  if (!plan || !seq_lens || !cu_new || (!pieces_out && max_pieces > 0)) return -PA_ERR_NULL;
+  if (num_seqs < 1 || num_seqs > plan->desc.max_seqs || num_tokens < 1 || num_tokens > plan->desc.max_tokens) return -PA_ERR_SHAPE;
+  const pa::PagedArgs a = arrange(*plan, nullptr, 0, nullptr, nullptr, nullptr, seq_lens, cu_new, num_seqs, (int32_t)num_tokens,
+                                  shared_len >= 0 ? &shared_len : nullptr, nullptr, nullptr, nullptr);
+  pa::PagedShape s = a.shape;
+  const bool with = a.shared_len != nullptr;
+  s.shared = with ? pa::whole_pages(s, shared_len, plan->page_shift) : 0;
+  auto segment = [&](int i) {
+    return with && i == 0 ? pa::shared_segment(s, cu_new[num_seqs])
+                          : pa::own_segment(s, cu_new[i - with], cu_new[i - with + 1], seq_lens[i - with]);
+  };
+  int64_t total = 0, count = 0;
+  for (int i = 0; i < num_seqs + with; ++i) total += s.Hkv * segment(i).cost;
+  const int64_t share = pa::share_of(s, total);
+  const int32_t active = pa::div_small(total + share - 1, share);
+  for (int32_t w = 0; w < active; ++w) {
+    int64_t x = w * share, start = 0;
+    const int64_t end = x + share < total ? x + share : total;
+    int i = 0;
+    while (start + s.Hkv * segment(i).cost <= x) start += s.Hkv * segment(i++).cost;
+    while (x < end) {
+      const pa::Segment g = segment(i);
+      if (start + s.Hkv * g.cost <= x) {
+        start += s.Hkv * g.cost;
+        ++i;
+        continue;
+      }
+      const bool shared = with && i == 0;
+      const int32_t head = pa::div_small(x - start, g.cost), block = pa::block_at(g, x - start - head * g.cost);
+      const int64_t c0 = start + head * g.cost + pa::blocks_cost(g, block), c1 = c0 + g.first_cost + (int64_t)block * g.more_cost;
+      const pa::Piece p = pa::make_piece(s, g, shared, block, c0, c1, x, end < c1 ? end : c1);
+      if (count < max_pieces) {
+        const int64_t left = (int64_t)g.tokens * s.group - (int64_t)block * s.block_rows;
+        const int64_t k1 = g.key0 + (int64_t)p.tile1 * s.tile_keys;
+        const int32_t row[8] = {w, shared ? -1 : i - (int)with, head, block * s.block_rows, (int32_t)(left < s.block_rows ? left : s.block_rows),
+                                g.key0 + p.tile0 * s.tile_keys, (int32_t)(k1 < p.key_end ? k1 : p.key_end), p.whole};
+        for (int e = 0; e < 8; ++e) pieces_out[count * 8 + e] = row[e];
+      }
+      ++count;
+      x = end < c1 ? end : c1;
+    }
+  }
+  return count;
+}
+
 }  // extern "C"

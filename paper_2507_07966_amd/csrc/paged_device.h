@@ -64,7 +64,7 @@ __device__ inline void write_row(const Place& p, int ch, mt::f32x4 v) {
 
 __device__ inline int32_t shared_keys(const PagedArgs& a) {
   if (!a.shared_len) return 0;
-  return (int32_t)clamp64(read_const(a.shared_len, 0), 0, a.shape.capacity) & ~((1 << a.page_shift) - 1);  // whole pages
+  return whole_pages(a.shape, read_const(a.shared_len, 0), a.page_shift);
 }
 __device__ inline Segment load_segment(const PagedArgs& a, const PagedShape& s, int i) {
   const int with = a.shared_len ? 1 : 0;

@@ -91,6 +91,11 @@ PA_HD Segment shared_segment(const PagedShape& s, int64_t cu_end) {
   return make_segment(s, 0, s.shared > 0 ? clamp64(cu_end, 0, s.T) : 0, s.shared - 1, 0, s.shared, 0);
 }
 
+// What a call takes as shared: whole pages, within the table.
+PA_HD int32_t whole_pages(const PagedShape& s, int32_t shared_len, int32_t page_shift) {
+  return (int32_t)clamp64(shared_len, 0, s.capacity) & ~((1 << page_shift) - 1);
+}
+
 // Keys [key0, end) that the rows of a block see, one past the table included: it has no page and makes its rows NaN.
 PA_HD int32_t block_key_end(const PagedShape& s, const Segment& g, bool shared, int32_t block) {
   if (shared) return s.shared;

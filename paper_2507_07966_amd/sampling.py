@@ -8,6 +8,8 @@ from __future__ import annotations
 import ctypes
 from typing import Optional, Sequence
 
+import numpy as np
+
 from . import binding
 from .binding import PA_BF16, PA_F32, PrefixAttnError, _stream
 
@@ -16,7 +18,7 @@ LAYOUTS = {"halves": 0, "pairs": 1}         # pa_rope_layout_t
 _DTYPES = {"f32": PA_F32, "bf16": PA_BF16}
 _SHAPE, _UNSUPPORTED = 2, 3                 # PA_ERR_SHAPE, PA_ERR_UNSUPPORTED
 EXPORTED_SYMBOLS = ("rope_axes_forward", "rope_axes_backward", "paged_attn_plan", "paged_attn_destroy", "paged_kv_append",
-                    "paged_kv_append_rope", "paged_attn_forward")
+                    "paged_kv_append_rope", "paged_attn_forward", "paged_attn_schedule", "paged_attn_schedule_shape")
 _lib = None
 _torch = None
 _code = {}                                  # torch dtype -> pa_dtype_t
@@ -50,6 +52,10 @@ def _load():
             "paged_kv_append_rope": [vp, ctypes.POINTER(_RopeDesc), vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, *call, vp],
             "paged_attn_forward": [vp, vp, i64, vp, vp, *call, vp, vp, vp, vp, sz, vp]}.items():
         getattr(lib, name).restype, getattr(lib, name).argtypes = ctypes.c_int, args
+    lib.paged_attn_schedule.restype = i64
+    lib.paged_attn_schedule.argtypes = [vp, vp, vp, i32, i64, i32, vp, i64]
+    lib.paged_attn_schedule_shape.restype = ctypes.c_int
+    lib.paged_attn_schedule_shape.argtypes = [vp, i32, i64, i32, *[ctypes.POINTER(i32)] * 3]
     lib.paged_attn_destroy.restype, lib.paged_attn_destroy.argtypes = None, [vp]
     _torch = torch
     _code.update({torch.float32: PA_F32, torch.bfloat16: PA_BF16})
@@ -181,6 +187,27 @@ class PagedAttnPlan:
         if self._h is None:
             raise ValueError("plan was destroyed")
         return self._h
+
+    def schedule(self, seq_lens, cu_new, num_tokens: int, shared_len: int = -1) -> np.ndarray:
+        """The pieces of work that paged_attn_forward's workgroups take for these lengths (host arrays; shared_len -1: not given): int32
+        [n, 8] = (share, sequence (-1: the shared keys), kv head, first stacked row, rows, first key, end of the keys, whole block)."""
+        lib = _lib or _load()
+        lens, cu = np.ascontiguousarray(seq_lens, dtype=np.int32), np.ascontiguousarray(cu_new, dtype=np.int32)
+        args = self.handle, lens.ctypes.data, cu.ctypes.data, len(lens), int(num_tokens), int(shared_len)
+        n = lib.paged_attn_schedule(*args, None, 0)
+        if n < 0:
+            raise PrefixAttnError(-n, "paged_attn_schedule")
+        out = np.zeros((n, 8), dtype=np.int32)
+        lib.paged_attn_schedule(*args, out.ctypes.data, n)
+        return out
+
+    def schedule_shape(self, num_seqs: int, num_tokens: int, shared: bool = False):
+        """Workgroups of such a call, rows of a block and keys of a tile."""
+        v = [ctypes.c_int32() for _ in range(3)]
+        st = (_lib or _load()).paged_attn_schedule_shape(self.handle, int(num_seqs), int(num_tokens), int(shared), *map(ctypes.byref, v))
+        if st:
+            raise PrefixAttnError(st, "paged_attn_schedule_shape")
+        return tuple(x.value for x in v)
 
     def destroy(self):
         if self._h is not None:
