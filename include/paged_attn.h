@@ -74,7 +74,7 @@ int rope_axes_backward(const rope_axes_desc_t* desc, int32_t dtype, const void* 
  * seq_lens[b] - n .. seq_lens[b] - 1.  Packed rows behind cu_new[num_seqs] are padding: nothing is computed for
  * them, and what is there stays.
  * These four arrays are int32 DEVICE memory and are checked by the kernels: no entry of them makes a call read or write
- * outside the caches and the packed rows. */
+ * outside the caches and the packed rows (where cu_new falls, paged_attn_forward computes nothing). */
 typedef struct paged_attn_plan paged_attn_plan_t; /* opaque, library-owned; host data only */
 
 typedef struct {

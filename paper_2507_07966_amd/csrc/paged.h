@@ -37,8 +37,7 @@ struct PagedCut {
 };
 // What workgroup 0 tells the merge about the line.
 struct PagedLine {
-  int64_t share;
-  int32_t active, shared;
+  int32_t share, active, shared;
 };
 
 struct PagedArgs {
@@ -51,11 +50,11 @@ struct PagedArgs {
   int32_t dtype, D, Hq, table_width, page_shift;
   float scale;
   PagedShape shape;        // `shared` is read on the device
-  int32_t groups, xcds;    // workgroups, and over how many XCDs they are laid out
+  int32_t groups, xcd_shift;  // workgroups, and log2 of the XCDs that they are laid out over
   int32_t blocks16;        // few rows: 16-row blocks of a block
   // workspace
   PagedLine* line;
-  int64_t* seg_start;      // [B + 2] cost at which segment i begins (with shared keys only: segment 0 is theirs)
+  int32_t* seg_start;      // [B + 2] cost at which segment i begins (with shared keys only: segment 0 is theirs)
   PagedCut* cuts;          // [groups]
   float* slots;            // [2 * groups][block_rows][D] fp32 partial outputs: of the block that share i continues (2 i) and
   float* slot_lse;         //   of the one that it begins and does not end (2 i + 1); [2 * groups][block_rows]
@@ -63,8 +62,8 @@ struct PagedArgs {
   float* rows_lse;         // [2][T * Hq]
 };
 int launch_paged_rows(const PagedArgs& a, void* stream);   // calls of few rows a sequence, and fp32
-int paged_rows_tile_keys(int32_t dtype, int32_t D);        // keys that its wavefronts share out in a step
-constexpr int PAGED_CHUNK_ROWS = 256, PAGED_CHUNK_KEYS = 64;
+int paged_rows_tile_shift(int32_t dtype, int32_t D);       // log2 of the keys that its wavefronts share out in a step
+constexpr int PAGED_CHUNK_ROWS = 256, PAGED_CHUNK_TILE_SHIFT = 6;
 int launch_paged_chunk(const PagedArgs& a, void* stream);  // bf16 calls of many rows a sequence
 int launch_paged_merge(const PagedArgs& a, void* stream);
 
@@ -73,7 +72,7 @@ int launch_paged_merge(const PagedArgs& a, void* stream);
 struct paged_attn_plan {
   paged_attn_desc_t desc;
   int32_t page_shift = 0;
-  int32_t num_cu = 256, num_xcd = 8;
+  int32_t num_cu = 256, xcd_shift = 3;
   int32_t group = 1;
   // workspace: byte offsets
   size_t off_seg_start = 0, off_cuts = 0, off_slot_lse = 0, off_slots = 0, off_rows_lse = 0, off_rows = 0, ws_bytes = 0;

@@ -182,7 +182,7 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   a.shared_len = rows <= FEW_ROWS * num_seqs ? shared_len : nullptr;
   a.blocks16 = blocks16_for(a.shared_len ? rows : (rows + num_seqs - 1) / num_seqs, d.dtype);
   a.groups = plan.num_cu;
-  a.xcds = plan.num_xcd;
+  a.xcd_shift = plan.xcd_shift;
   pa::PagedShape& s = a.shape;
   s.B = num_seqs;
   s.T = num_tokens;
@@ -190,16 +190,21 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   s.group = plan.group;
   const bool chunk = is_chunk(rows, num_seqs, d.dtype);
   s.block_rows = chunk ? pa::PAGED_CHUNK_ROWS : 16 * a.blocks16;
-  s.tile_keys = chunk ? pa::PAGED_CHUNK_KEYS : pa::paged_rows_tile_keys(d.dtype, d.head_dim);
+  s.tile_shift = chunk ? pa::PAGED_CHUNK_TILE_SHIFT : pa::paged_rows_tile_shift(d.dtype, d.head_dim);
   s.causal_cuts = chunk;
-  s.block_tokens = s.block_rows / s.group;
-  s.inv_groups = 1.0 / a.groups;
   s.inv_group = 1.0f / (float)s.group;
   s.capacity = d.max_pages_per_seq << plan.page_shift;
-  s.start_keys = chunk ? CHUNK_START_KEYS : START_KEYS;
-  s.min_share = chunk ? CHUNK_MIN_SHARE : MIN_SHARE;
+  const int32_t start = chunk ? CHUNK_START_KEYS : START_KEYS, least = chunk ? CHUNK_MIN_SHARE : MIN_SHARE;
+  // No lengths of such a call can cost more than this many keys; the unit keeps that below 2^30 units.
+  const double most = ((double)rows / s.block_rows + 2.0 * (num_seqs + 1)) * s.Hkv * ((double)s.capacity + num_tokens + start + 64);
+  s.unit_shift = 4;
+  while (most / (double)((int64_t)1 << s.unit_shift) > (double)(1 << 29)) ++s.unit_shift;
+  s.start_cost = (start >> s.unit_shift) + 1;
+  s.min_share = (least >> s.unit_shift) + 1;
+  s.more_cost = (s.block_rows / s.group) >> s.unit_shift;
+  s.per_group = (1.0f + 1.0f / (1 << 20)) / (float)a.groups;
   a.line = reinterpret_cast<pa::PagedLine*>(ws);
-  a.seg_start = reinterpret_cast<int64_t*>(ws + plan.off_seg_start);
+  a.seg_start = reinterpret_cast<int32_t*>(ws + plan.off_seg_start);
   a.cuts = reinterpret_cast<pa::PagedCut*>(ws + plan.off_cuts);
   a.slot_lse = reinterpret_cast<float*>(ws + plan.off_slot_lse);
   a.slots = reinterpret_cast<float*>(ws + plan.off_slots);
@@ -255,7 +260,7 @@ int paged_attn_plan(const paged_attn_desc_t* desc, paged_attn_plan_t** plan_out,
       return PA_ERR_HIP;
     }
     p->num_cu = n;
-    p->num_xcd = n == 256 ? 8 : 1;  // the layout that shares are spread over XCDs for
+    p->xcd_shift = n == 256 ? 3 : 0;  // the layout that shares are spread over XCDs for
   }
   // What the shares leave of blocks that they cut, and, where shared keys are a segment of their own, partials of all rows.
   const int64_t block_rows = is_chunk(d.max_tokens * p->group, 1, d.dtype) ? pa::PAGED_CHUNK_ROWS : 64, slots = 2 * (int64_t)p->num_cu * block_rows;
@@ -266,7 +271,7 @@ int paged_attn_plan(const paged_attn_desc_t* desc, paged_attn_plan_t** plan_out,
     at += (bytes + 255) / 256 * 256;
     return off;
   };
-  p->off_seg_start = take(((size_t)d.max_seqs + 2) * sizeof(int64_t));
+  p->off_seg_start = take(((size_t)d.max_seqs + 2) * sizeof(int32_t));
   p->off_cuts = take((size_t)p->num_cu * sizeof(pa::PagedCut));
   p->off_slot_lse = take((size_t)slots * sizeof(float));
   p->off_slots = take((size_t)slots * d.head_dim * sizeof(float));
@@ -329,7 +334,7 @@ int paged_attn_schedule_shape(const paged_attn_plan_t* plan, int32_t num_seqs, i
                                   with_shared ? &given : nullptr, nullptr, nullptr, nullptr);
   *groups = a.groups;
   *block_rows = a.shape.block_rows;
-  *tile_keys = a.shape.tile_keys;
+  *tile_keys = 1 << a.shape.tile_shift;
   return PA_OK;
 }
 
@@ -346,15 +351,17 @@ int64_t paged_attn_schedule(const paged_attn_plan_t* plan, const int32_t* seq_le
     return with && i == 0 ? pa::shared_segment(s, cu_new[num_seqs])
                           : pa::own_segment(s, cu_new[i - with], cu_new[i - with + 1], seq_lens[i - with]);
   };
-  int64_t total = 0, count = 0;
-  for (int i = 0; i < num_seqs + with; ++i) total += s.Hkv * segment(i).cost;
-  const int64_t share = pa::share_of(s, total);
-  const int32_t active = pa::div_small(total + share - 1, share);
+  int64_t count = 0;
+  int32_t total = 0;
+  for (int i = 0; i < num_seqs + with; ++i) {
+    const int32_t cost = segment(i).cost;
+    if (cost < 0) return 0;
+    total += s.Hkv * cost;
+  }
+  const int32_t share = pa::share_of(s, total), active = pa::active_of(total, share);
   for (int32_t w = 0; w < active; ++w) {
-    int64_t x = w * share, start = 0;
-    const int64_t end = x + share < total ? x + share : total;
-    int i = 0;
-    while (start + s.Hkv * segment(i).cost <= x) start += s.Hkv * segment(i++).cost;
+    int32_t x = w * share, start = 0, i = 0;
+    const int32_t end = x + share < total ? x + share : total;
     while (x < end) {
       const pa::Segment g = segment(i);
       if (start + s.Hkv * g.cost <= x) {
@@ -363,18 +370,17 @@ int64_t paged_attn_schedule(const paged_attn_plan_t* plan, const int32_t* seq_le
         continue;
       }
       const bool shared = with && i == 0;
-      const int32_t head = pa::div_small(x - start, g.cost), block = pa::block_at(g, x - start - head * g.cost);
-      const int64_t c0 = start + head * g.cost + pa::blocks_cost(g, block), c1 = c0 + g.first_cost + (int64_t)block * g.more_cost;
-      const pa::Piece p = pa::make_piece(s, g, shared, block, c0, c1, x, end < c1 ? end : c1);
+      const int32_t head = pa::div_small(x - start, g.cost), head_start = start + head * g.cost, block = pa::block_at(g, x - head_start);
+      const pa::Block b = pa::make_block(s, g, head_start, block);
+      const pa::Piece p = pa::make_piece(s, g, shared, b, x, end);
       if (count < max_pieces) {
-        const int64_t left = (int64_t)g.tokens * s.group - (int64_t)block * s.block_rows;
-        const int64_t k1 = g.key0 + (int64_t)p.tile1 * s.tile_keys;
-        const int32_t row[8] = {w, shared ? -1 : i - (int)with, head, block * s.block_rows, (int32_t)(left < s.block_rows ? left : s.block_rows),
-                                g.key0 + p.tile0 * s.tile_keys, (int32_t)(k1 < p.key_end ? k1 : p.key_end), p.whole};
+        const int32_t k1 = g.key0 + (p.tile1 << s.tile_shift);
+        const int32_t row[8] = {w, shared ? -1 : i - (int)with, head, block * s.block_rows, b.rows, g.key0 + (p.tile0 << s.tile_shift),
+                                k1 < p.key_end ? k1 : p.key_end, p.whole};
         for (int e = 0; e < 8; ++e) pieces_out[count * 8 + e] = row[e];
       }
       ++count;
-      x = end < c1 ? end : c1;
+      x = end < b.c1 ? end : b.c1;
     }
   }
   return count;

@@ -27,7 +27,7 @@ namespace {
 using namespace mt;
 
 constexpr int NQ = 2, WAVES = 8, THREADS = WAVES * 64, ROWS_PER_WAVE = 16 * NQ, ROWS = WAVES * ROWS_PER_WAVE;
-static_assert(ROWS == PAGED_CHUNK_ROWS && TILE == PAGED_CHUNK_KEYS, "the schedule's blocks and tiles");
+static_assert(ROWS == PAGED_CHUNK_ROWS && TILE == 1 << PAGED_CHUNK_TILE_SHIFT, "the schedule's blocks and tiles");
 constexpr float SAFE_SUM = 65536.0f;  // a lane's sum of a tile's probabilities below this keeps fp32 and bf16 far from overflow
 constexpr int RING = 4;               // LDS operand reads ahead of the MFMAs that use them
 
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
   for (; walk.more(); walk.next(a)) {
     const Piece p = walk.piece();
     const Segment& seg = walk.seg;
-    const int block_rows = walk.rows();
+    const int block_rows = walk.block.rows;
     const int32_t* const table = a.page_table + (int64_t)walk.table_row * a.table_width;
     const int first_key = seg.key0 + p.tile0 * TILE, tiles = p.tile1 - p.tile0;
 
@@ -82,8 +82,8 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
       limit[nq] = 0x7fffffff;
       if (r < block_rows) {
         const int tok = walk.row_token(r);
-        row = static_cast<const __bf16*>(a.q) + (int64_t)(walk.token + tok) * a.q_stride + walk.row_head(r, tok) * D + 8 * g4;
-        limit[nq] = (int)clamp64(seg.first_pos + (walk.token - seg.token0) + tok, -1, shape.capacity);
+        row = static_cast<const __bf16*>(a.q) + (int64_t)(seg.token0 + tok) * a.q_stride + walk.row_head(r, tok) * D + 8 * g4;
+        limit[nq] = row_limit(shape, seg, tok);
       }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) Q[nq][ks] = row ? *reinterpret_cast<const bf16x8*>(row + 32 * ks) : bf16x8{0, 0, 0, 0, 0, 0, 0, 0};

@@ -35,11 +35,6 @@ __device__ inline void wait_loads() {
 }
 __device__ inline void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-__device__ inline int64_t uniform64(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
 // Lengths, tables and the like: nothing writes them while a kernel runs, which the address space says, so that uniform reads are scalar.
 __device__ inline int32_t read_const(const int32_t* p, int64_t i) {
   typedef const __attribute__((address_space(4))) int32_t* Const;
@@ -72,18 +67,24 @@ __device__ inline Segment load_segment(const PagedArgs& a, const PagedShape& s, 
   return own_segment(s, read_const(a.cu_new, i - with), read_const(a.cu_new, i - with + 1), read_const(a.seq_lens, i - with));
 }
 
+// The last key that a new token sees, at most the one behind the table; -1: none.
+__device__ inline int32_t row_limit(const PagedShape& s, const Segment& g, int32_t token) {
+  const int32_t pos = g.first_pos + token;
+  return pos < 0 ? -1 : pos < s.capacity ? pos : s.capacity;
+}
+
 // A workgroup's way along its share: one piece of a block at a time.  All members are uniform.
 struct Walk {
   PagedShape shape;
   Segment seg;
-  int32_t seg_index, segments, head, block;
+  Block block;
+  int32_t seg_index, segments, head, block_index;
+  int32_t head_start;  // where the kv head's blocks begin on the line
+  int32_t x, x_end;    // what is left of the share
+  int32_t share, position;
   int32_t table_row;   // of the page table
   int32_t first_seq;   // the first sequence with new tokens: shared keys are read through its row
-  int32_t position;    // number of the share
   bool shared;         // the segment is that of the shared keys
-  int64_t seg_start, x, x_end, share;
-  int32_t token, row_in_group;  // of the block's first row: packed token and index among its group's rows
-  int64_t c0, c1;               // the block's place on the line
 
   __device__ bool more() const { return x < x_end; }
   __device__ void enter(const PagedArgs& a) {
@@ -91,49 +92,41 @@ struct Walk {
     table_row = shared ? first_seq : seg_index - (a.shared_len ? 1 : 0);
   }
   __device__ Piece piece() {
-    c0 = seg_start + head * seg.cost + blocks_cost(seg, block);
-    c1 = c0 + seg.first_cost + (int64_t)block * seg.more_cost;
-    const uint32_t row0 = (uint32_t)(block * shape.block_rows), i = row0 / (uint32_t)shape.group;
-    token = seg.token0 + i;
-    row_in_group = row0 - i * shape.group;
-    return make_piece(shape, seg, shared, block, c0, c1, x, x_end < c1 ? x_end : c1);
+    block = make_block(shape, seg, head_start, block_index);
+    return make_piece(shape, seg, shared, block, x, x_end);
   }
-  // Rows of the block, and the token (counted from the block's first) and the query head of its row r.
-  __device__ int32_t rows() const {
-    const int32_t left = seg.tokens * shape.group - block * shape.block_rows;
-    return left < shape.block_rows ? left : shape.block_rows;
-  }
-  __device__ int32_t row_token(int32_t r) const { return group_of(shape, row_in_group + r); }
-  __device__ int32_t row_head(int32_t r, int32_t tok) const { return head * shape.group + row_in_group + r - tok * shape.group; }
   __device__ void next(const PagedArgs& a) {
-    x = x_end < c1 ? x_end : c1;
+    x = x_end < block.c1 ? x_end : block.c1;
     if (x >= x_end) return;
-    if (++block < seg.blocks) return;
-    block = 0;
+    if (++block_index < seg.blocks) return;
+    block_index = 0;
+    head_start += seg.cost;
     if (++head < shape.Hkv) return;
     head = 0;
     do {
-      seg_start += shape.Hkv * seg.cost;
       seg = load_segment(a, shape, ++seg_index);  // there is one more with work: x < x_end
     } while (seg.cost == 0 && seg_index + 1 < segments);
     enter(a);
   }
+  // The token (counted from the segment's first) and the query head of the block's row r.
+  __device__ int32_t row_token(int32_t r) const { return block.token + group_of(shape, block.row + r); }
+  __device__ int32_t row_head(int32_t r, int32_t tok) const { return head * shape.group + block.row + r - (tok - block.token) * shape.group; }
   __device__ Place place(const PagedArgs& a, const Piece& p, int r) const {
-    const int32_t tok = row_token(r);
-    const int64_t t = token + tok, h = row_head(r, tok);
-    if (p.whole && !a.shared_len)
-      return Place{static_cast<char*>(a.out) + (t * a.Hq + h) * a.D * (a.dtype == PA_BF16 ? 2 : 4), a.lse ? a.lse + h * shape.T + t : nullptr, false};
-    if (p.whole) {
-      const int64_t row = ((shared ? (int64_t)shape.T : 0) + t) * a.Hq + h;
-      return Place{a.rows + row * a.D, a.rows_lse + row, true};
+    if (!p.whole) {
+      const int64_t row = (2 * position + (x == block.c0 ? 1 : 0)) * shape.block_rows + r;
+      return Place{a.slots + row * a.D, a.slot_lse + row, true};
     }
-    const int64_t row = (2 * (int64_t)position + (x == c0 ? 1 : 0)) * shape.block_rows + r;
-    return Place{a.slots + row * a.D, a.slot_lse + row, true};
+    const int32_t tok = row_token(r);
+    const int64_t t = seg.token0 + tok, h = row_head(r, tok);
+    if (!a.shared_len)
+      return Place{static_cast<char*>(a.out) + (t * a.Hq + h) * a.D * (a.dtype == PA_BF16 ? 2 : 4), a.lse ? a.lse + h * shape.T + t : nullptr, false};
+    const int64_t row = ((shared ? (int64_t)shape.T : 0) + t) * a.Hq + h;
+    return Place{a.rows + row * a.D, a.rows_lse + row, true};
   }
   // Thread 0 notes for the merge a block that this share begins and does not end.
   __device__ void note_cut(const PagedArgs& a) const {
-    if (threadIdx.x == 0 && x == c0 && x_end < c1)
-      a.cuts[position] = PagedCut{seg.token0, seg.tokens, head, block, position, div_small(c1 - 1, share)};
+    if (threadIdx.x == 0 && x == block.c0 && x_end < block.c1)
+      a.cuts[position] = PagedCut{seg.token0, seg.tokens, head, block_index, position, div_small(block.c1 - 1, share)};
   }
 };
 
@@ -141,19 +134,21 @@ struct Walk {
 template <int THREADS>
 __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   constexpr int WAVES = THREADS / 64;
-  __shared__ int64_t wave_cost[WAVES];
-  __shared__ int64_t found_start;
+  __shared__ int32_t wave_cost[WAVES], found_start;
   __shared__ Segment found;
-  __shared__ int32_t found_segment, first_seq;
+  __shared__ int32_t found_segment, first_seq, falls;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   w.shape = a.shape;
   w.shape.shared = shared_keys(a);
   const int with = a.shared_len ? 1 : 0;
   w.segments = a.shape.B + with;
-  if (tid == 0) first_seq = 0x7fffffff;
+  if (tid == 0) {
+    first_seq = 0x7fffffff;
+    falls = 0;
+  }
   __syncthreads();
   // Two rounds over the segments where they are more than the threads: the sum of all costs, then the share's segment.
-  int64_t total = 0, start = 0, cost = 0;
+  int32_t total = 0, start = 0, cost = 0;
   Segment g;
   const int lanes = w.segments < 64 ? w.segments : 64;
   auto round = [&](int base) {  // start and cost of segment base + tid; total: those before base, and then with this round's
@@ -161,17 +156,18 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
     cost = 0;
     if (i < w.segments) {
       g = load_segment(a, w.shape, i);
-      cost = w.shape.Hkv * g.cost;
+      if (g.cost < 0) falls = 1;
+      cost = g.cost < 0 ? 0 : w.shape.Hkv * g.cost;
       if (i >= with && cost > 0) atomicMin(&first_seq, i - with);
     }
-    int64_t sum = cost;
+    int32_t sum = cost;
     for (int d = 1; d < lanes; d *= 2) {
-      const int64_t up = __shfl_up((long long)sum, d);
+      const int32_t up = __shfl_up(sum, d);
       if (lane >= d) sum += up;
     }
     if (lane == lanes - 1) wave_cost[wave] = sum;
     __syncthreads();
-    int64_t before = 0, all = 0;
+    int32_t before = 0, all = 0;
 #pragma unroll
     for (int v = 0; v < WAVES; ++v) {
       before += v < wave ? wave_cost[v] : 0;
@@ -185,11 +181,11 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
     round(base);
     if (blockIdx.x == 0 && with && base + tid < w.segments) a.seg_start[base + tid] = start;
   }
-  total = uniform64(total);
+  total = __builtin_amdgcn_readfirstlane(falls ? 0 : total);
   w.share = share_of(w.shape, total);
-  const int32_t active = div_small(total + w.share - 1, w.share);
+  const int32_t active = active_of(total, w.share);
   if (blockIdx.x == 0 && tid == 0) *a.line = PagedLine{w.share, active, w.shape.shared};
-  w.position = position_of(blockIdx.x, active, a.xcds);
+  w.position = position_of(blockIdx.x, active, a.xcd_shift);
   if (w.position < 0) return false;
   w.x = w.position * w.share;
   w.x_end = w.x + w.share < total ? w.x + w.share : total;
@@ -204,19 +200,19 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   }
   __syncthreads();
   w.seg_index = __builtin_amdgcn_readfirstlane(found_segment);
-  w.seg_start = uniform64(found_start);
   w.first_seq = __builtin_amdgcn_readfirstlane(first_seq < a.shape.B ? first_seq : a.shape.B - 1);
   w.seg.token0 = __builtin_amdgcn_readfirstlane(found.token0);
   w.seg.tokens = __builtin_amdgcn_readfirstlane(found.tokens);
   w.seg.key0 = __builtin_amdgcn_readfirstlane(found.key0);
   w.seg.blocks = __builtin_amdgcn_readfirstlane(found.blocks);
-  w.seg.first_pos = uniform64(found.first_pos);
+  w.seg.first_pos = __builtin_amdgcn_readfirstlane(found.first_pos);
   w.seg.first_cost = __builtin_amdgcn_readfirstlane(found.first_cost);
   w.seg.more_cost = __builtin_amdgcn_readfirstlane(found.more_cost);
-  w.seg.cost = uniform64(found.cost);
-  const int64_t off = w.x - w.seg_start;
-  w.head = __builtin_amdgcn_readfirstlane(div_small(off, w.seg.cost));
-  w.block = __builtin_amdgcn_readfirstlane(block_at(w.seg, off - w.head * w.seg.cost));
+  w.seg.cost = __builtin_amdgcn_readfirstlane(found.cost);
+  const int32_t seg_start = __builtin_amdgcn_readfirstlane(found_start);
+  w.head = __builtin_amdgcn_readfirstlane(div_small(w.x - seg_start, w.seg.cost));
+  w.head_start = seg_start + w.head * w.seg.cost;
+  w.block_index = __builtin_amdgcn_readfirstlane(block_at(w.seg, w.x - w.head_start));
   w.enter(a);
   if (tid == 0) a.cuts[w.position] = PagedCut{0, 0, 0, 0, 0, 0};
   return true;

@@ -131,6 +131,7 @@ __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) 
   __shared__ int seq;
   const int64_t t = blockIdx.x;
   const int64_t h = blockIdx.y;
+  if (a.line->active == 0) return;
   if (threadIdx.x == 0) seq = -1;
   __syncthreads();
   for (int b = threadIdx.x; b < a.shape.B; b += THREADS)
@@ -140,12 +141,12 @@ __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) 
   if (b < 0) return;
   PagedShape s = a.shape;
   s.shared = a.line->shared;
-  const int64_t share = a.line->share;
+  const int32_t share = a.line->share;
   const int head = (int)h / s.group, j = (int)h - head * s.group;
-  auto pieces = [&](const Segment& g, int64_t start, bool shared) {
+  auto pieces = [&](const Segment& g, int32_t start, bool shared) {
     const uint32_t m = (uint32_t)(t - g.token0) * s.group + j;
     const int block = (int)(m / (uint32_t)s.block_rows), r = (int)(m - (uint32_t)block * s.block_rows);
-    const int64_t c0 = start + head * g.cost + blocks_cost(g, block), c1 = c0 + g.first_cost + block * g.more_cost;
+    const int32_t c0 = start + head * g.cost + blocks_cost(g, block), c1 = c0 + g.first_cost + block * g.more_cost;
     const int32_t first = div_small(c0, share), last = div_small(c1 - 1, share);
     if (first == last) return Pieces{1, ((shared ? (int64_t)s.T : 0) + t) * a.Hq + h, true, first, r};
     return Pieces{last - first + 1, (2 * (int64_t)first + 1) * s.block_rows + r, false, first, r};

@@ -184,7 +184,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
   constexpr int GROUP_LOADS = 16 * ROWB / 1024;  // 1 KiB loads of 16 keys
   constexpr int LANES_PER_ROW = ROWB / 16, ROWS_PER_LOAD = 1024 / ROWB;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[WAVES * STAGES * 2 * HALF_STAGE];
-  __shared__ float wave_max[WAVES][ROWS], wave_sum[WAVES][ROWS];
+  __shared__ float wave_max[WAVES][ROWS], wave_sum[WAVES][ROWS], row_scale[ROWS];
   constexpr int VECS = D / 4;  // 16-byte pieces of a row of fp32
   static_assert(WAVES * ROWS * D * 4 <= (int)sizeof(ring), "the joint fits the ring");
 
@@ -209,10 +209,10 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
   for (; walk.more(); walk.next(a)) {
     const Piece p = walk.piece();
     const Segment& seg = walk.seg;
-    const int block_rows = walk.rows();
+    const int block_rows = walk.block.rows;
     const int32_t* const table = a.page_table + (int64_t)walk.table_row * a.table_width;
-    const int first_key = seg.key0 + p.tile0 * shape.tile_keys;
-    const int last_key = p.tile1 * shape.tile_keys + seg.key0 < p.key_end ? p.tile1 * shape.tile_keys + seg.key0 : p.key_end;
+    const int first_key = seg.key0 + (p.tile0 << shape.tile_shift);
+    const int last_key = (p.tile1 << shape.tile_shift) + seg.key0 < p.key_end ? (p.tile1 << shape.tile_shift) + seg.key0 : p.key_end;
     // stages of this wavefront: stage s covers keys first_key + (WAVES s + wave) KEYS ..
     const int span = last_key - first_key - wave * KEYS;
     const int stages = span > 0 ? (span + WAVES * KEYS - 1) / (WAVES * KEYS) : 0;
@@ -262,8 +262,8 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       limit[nq] = 0x7fffffff;
       if (r < block_rows) {
         const int tok = walk.row_token(r);
-        row = static_cast<const T*>(a.q) + (int64_t)(walk.token + tok) * a.q_stride + walk.row_head(r, tok) * D;
-        if (!walk.shared) limit[nq] = (int)clamp64(seg.first_pos + (walk.token - seg.token0) + tok, -1, shape.capacity);
+        row = static_cast<const T*>(a.q) + (int64_t)(seg.token0 + tok) * a.q_stride + walk.row_head(r, tok) * D;
+        if (!walk.shared) limit[nq] = row_limit(shape, seg, tok);
       }
       core.load_q(nq, row, g4);
       least = limit[nq] < least ? limit[nq] : least;
@@ -380,22 +380,23 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       for (int w = 0; w < WAVES; ++w) m = fmaxf(m, wave_max[w][r]);
       if (r < block_rows) core.store(joint + (wave * ROWS + r) * VECS, nq, factor(top[nq], m), g4, l16);
     }
+    if (tid < block_rows) {
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) m = fmaxf(m, wave_max[w][tid]);
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) l += wave_sum[w][tid] * factor(wave_max[w][tid], m);
+      row_scale[tid] = l == 0.f ? 0.f : 1.f / l;  // 0: no key is seen
+      const Place dst = walk.place(a, p, tid);
+      if (dst.lse) *dst.lse = m * a.scale + __logf(l);
+    }
     __syncthreads();
     for (int idx = tid; idx < block_rows * VECS; idx += THREADS) {
       const int r = idx / VECS, v = idx % VECS;
-      float m = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) m = fmaxf(m, wave_max[w][r]);
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        l += wave_sum[w][r] * factor(wave_max[w][r], m);
-        o += joint[(w * ROWS + r) * VECS + (v ^ (r & 15))];
-      }
-      const float inv = l == 0.f ? 0.f : 1.f / l;  // 0: no key is seen
-      const Place dst = walk.place(a, p, r);
-      write_row<T>(dst, 4 * v, o * inv);
-      if (v == 0 && dst.lse) *dst.lse = m * a.scale + __logf(l);
+      for (int w = 0; w < WAVES; ++w) o += joint[(w * ROWS + r) * VECS + (v ^ (r & 15))];
+      write_row<T>(walk.place(a, p, r), 4 * v, o * row_scale[r]);
     }
     walk.note_cut(a);
     __syncthreads();  // the joint is read before the next block's loads come
@@ -421,6 +422,10 @@ int launch_paged_rows(const PagedArgs& a, void* stream) {
   return (int)hipGetLastError();
 }
 
-int paged_rows_tile_keys(int32_t dtype, int32_t D) { return WAVES * HALF_STAGE / (D * (dtype == PA_BF16 ? 2 : 4)); }
+int paged_rows_tile_shift(int32_t dtype, int32_t D) {
+  int shift = 0;
+  while ((D * (dtype == PA_BF16 ? 2 : 4)) << shift < WAVES * HALF_STAGE) ++shift;
+  return shift;
+}
 
 }  // namespace pa
