@@ -40,6 +40,25 @@ def check_device_flag(hipcc: str, bdir: str) -> None:
         raise RuntimeError(f"the device compilation pass does not accept the build's flags:\n{r.stdout}")
 
 
+BINDING = os.path.join(HERE, "_sampling.so")
+
+
+def binding_commands(bdir: str):
+    """Compile and link commands of csrc/py_sampling.cpp, the Python module that checks the sampling calls' tensors: plain C++ against
+    torch's and Python's headers, linked to the library beside it."""
+    import sysconfig
+    import torch
+    base = os.path.join(os.path.dirname(torch.__file__))
+    obj, lib = os.path.join(bdir, "py_sampling.cpp.o"), os.path.join(base, "lib")
+    cc = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    compile_cmd = [*cc, "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+                   "-isystem", sysconfig.get_paths()["include"], f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}", "-Wall", "-c",
+                   os.path.join(CSRC, "py_sampling.cpp"), "-o", obj]
+    link_cmd = [*cc, "-shared", obj, "-o", BINDING, f"-L{HERE}", "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN", f"-L{lib}", "-ltorch_python",
+                "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{lib}"]
+    return compile_cmd, link_cmd
+
+
 def build(verbose: bool = False, extra_flags=(), out: str = LIB) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objs = []
@@ -56,6 +75,9 @@ def build(verbose: bool = False, extra_flags=(), out: str = LIB) -> str:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
+    if out == LIB:   # other outputs are builds of the library alone
+        compile_cmd, link_cmd = binding_commands(bdir)
+        procs.append(("py_sampling.cpp", subprocess.Popen(compile_cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = False
     for src, p in procs:
         log, _ = p.communicate()
@@ -69,6 +91,8 @@ def build(verbose: bool = False, extra_flags=(), out: str = LIB) -> str:
         raise RuntimeError("hipcc failed")
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", out]
     subprocess.run(cmd, check=True)
+    if out == LIB:
+        subprocess.run(link_cmd, check=True)
     return out
 
 

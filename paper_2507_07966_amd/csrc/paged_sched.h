@@ -16,7 +16,11 @@
 
 #include <cstdint>
 
+#if defined(__HIPCC__)
 #define PA_HD __host__ __device__ inline __attribute__((always_inline))
+#else
+#define PA_HD inline
+#endif
 
 namespace pa {
 

@@ -1,8 +1,9 @@
 """ctypes binding of the sampling phase (include/paged_attn.h): rotary positions with several axes, the paged cache of keys and
 values, and the attention of each sequence's newest tokens over its pages.
 
-Tensors are torch device tensors.  Their type, shape, device and strides are checked here and the numbers in the library; either
-way a call that cannot run raises PrefixAttnError before anything is enqueued.  There is no CPU fallback."""
+Tensors are torch device tensors.  Their types, shapes, devices and strides are checked by a small native module (csrc/py_sampling.cpp) and the
+numbers in the library; either way a call that cannot run raises PrefixAttnError before anything is enqueued.  There is no CPU
+fallback."""
 from __future__ import annotations
 
 import ctypes
@@ -20,8 +21,7 @@ _SHAPE, _UNSUPPORTED = 2, 3                 # PA_ERR_SHAPE, PA_ERR_UNSUPPORTED
 EXPORTED_SYMBOLS = ("rope_axes_forward", "rope_axes_backward", "paged_attn_plan", "paged_attn_destroy", "paged_kv_append",
                     "paged_kv_append_rope", "paged_attn_forward", "paged_attn_schedule", "paged_attn_schedule_shape")
 _lib = None
-_torch = None
-_code = {}                                  # torch dtype -> pa_dtype_t
+_native = None                              # the module built from csrc/py_sampling.cpp
 
 
 class _RopeDesc(ctypes.Structure):
@@ -37,55 +37,40 @@ class _PagedDesc(ctypes.Structure):
 
 
 def _load():
-    global _lib, _torch
+    global _lib
     if _lib is not None:
         return _lib
     lib = binding.load_library()
-    import torch
     i32, i64, vp, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
-    rope = [ctypes.POINTER(_RopeDesc), i32, vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, i64, vp, i64, vp]
-    call = [vp, vp, vp, i32, i64]            # page_table, seq_lens, cu_new, num_seqs, num_tokens
-    for name, args in {
-            "rope_axes_forward": rope, "rope_axes_backward": rope,
-            "paged_attn_plan": [ctypes.POINTER(_PagedDesc), ctypes.POINTER(vp), ctypes.POINTER(sz)],
-            "paged_kv_append": [vp, vp, i64, vp, i64, vp, vp, *call, vp],
-            "paged_kv_append_rope": [vp, ctypes.POINTER(_RopeDesc), vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, *call, vp],
-            "paged_attn_forward": [vp, vp, i64, vp, vp, *call, vp, vp, vp, vp, sz, vp]}.items():
-        getattr(lib, name).restype, getattr(lib, name).argtypes = ctypes.c_int, args
+    lib.paged_attn_plan.restype = ctypes.c_int
+    lib.paged_attn_plan.argtypes = [ctypes.POINTER(_PagedDesc), ctypes.POINTER(vp), ctypes.POINTER(sz)]
     lib.paged_attn_schedule.restype = i64
     lib.paged_attn_schedule.argtypes = [vp, vp, vp, i32, i64, i32, vp, i64]
     lib.paged_attn_schedule_shape.restype = ctypes.c_int
     lib.paged_attn_schedule_shape.argtypes = [vp, i32, i64, i32, *[ctypes.POINTER(i32)] * 3]
     lib.paged_attn_destroy.restype, lib.paged_attn_destroy.argtypes = None, [vp]
-    _torch = torch
-    _code.update({torch.float32: PA_F32, torch.bfloat16: PA_BF16})
     _lib = lib
     return lib
+
+
+def _load_native():
+    """Imports the module that checks the calls' tensors; raises if it has not been built (python -m paper_2507_07966_amd.build)."""
+    global _native
+    _load()   # torch and the library first: the module links to both
+    from . import _sampling
+    _native = _sampling
+    return _native
 
 
 def _refuse(status: int, where: str, what: str):
     raise PrefixAttnError(status, f"{where}: {what}")
 
 
-def _heads(where, name, x, tokens, heads, dim, dtype, device):
-    """x is [tokens, heads, dim], each token's heads contiguous; returns the distance of its tokens in elements."""
-    if x.dtype is not dtype or x.device != device:
-        _refuse(_UNSUPPORTED, where, f"{name} has to be {dtype} on {device}, not {x.dtype} on {x.device}")
-    if x.shape != (tokens, heads, dim):
-        _refuse(_SHAPE, where, f"{name} has to be [{tokens}, {heads}, {dim}], not {list(x.shape)}")
-    stride = x.stride()
-    if tokens and (stride[2] != 1 or (heads > 1 and stride[1] != dim)):
-        _refuse(_SHAPE, where, f"{name}'s heads have to be contiguous, its strides are {list(stride)}")
-    return stride[0] if tokens > 1 else heads * dim
-
-
-def _array(where, name, x, shape, dtype, device):
-    """x is a contiguous tensor of this shape and type."""
-    if x.dtype is not dtype or x.device != device:
-        _refuse(_UNSUPPORTED, where, f"{name} has to be {dtype} on {device}, not {x.dtype} on {x.device}")
-    if x.shape != shape or not x.is_contiguous():
-        _refuse(_SHAPE, where, f"{name} has to be a contiguous {list(shape)}, not {list(x.shape)} of strides {list(x.stride())}")
-    return x.data_ptr()
+def _check(where: str, refused) -> None:
+    """`refused`: None, or the status and the text that csrc/py_sampling.cpp returns for a call that was not enqueued."""
+    if refused is not None:
+        status, what = refused
+        raise PrefixAttnError(status, f"{where}: {what}" if what else where)
 
 
 class RopeAxes:
@@ -93,7 +78,7 @@ class RopeAxes:
 
     def __init__(self, desc: _RopeDesc):
         self._desc = desc
-        self._ref = ctypes.byref(desc)
+        self._address = ctypes.addressof(desc)
         self.head_dim, self.rotary_dim, self.num_axes = desc.head_dim, desc.rotary_dim, desc.num_axes
         self.layout = {v: k for k, v in LAYOUTS.items()}[desc.layout]
         self.pair_axis = tuple(desc.pair_axis[:desc.rotary_dim // 2])
@@ -130,48 +115,16 @@ def rope_axes(sections: Sequence[int], head_dim: int, rotary_dim: Optional[int] 
     return RopeAxes(d)
 
 
-def _current(where, device):
-    """The device has to be the current one: the calls enqueue on its stream."""
-    if device.type != "cuda" or device.index != _torch.cuda.current_device():
-        _refuse(_UNSUPPORTED, where, f"tensors have to be on the current GPU, not on {device}")
-
-
-def _rope_call(where, rope, q, k, positions, inv_freq, q_out, k_out, stream):
-    lib = _lib or _load()
-    dtype, device, dim = q.dtype, q.device, rope.head_dim
-    if dtype not in _code:
-        _refuse(_UNSUPPORTED, where, f"float32 or bfloat16, not {dtype}")
-    if q.dim() != 3:
-        _refuse(_SHAPE, where, f"q has to be [tokens, heads, {dim}], not {list(q.shape)}")
-    _current(where, device)
-    tokens, hq = q.shape[0], q.shape[1]
-    sq, sqo = _heads(where, "q", q, tokens, hq, dim, dtype, device), _heads(where, "q_out", q_out, tokens, hq, dim, dtype, device)
-    hk = sk = sko = 0
-    if (k is None) != (k_out is None):
-        _refuse(_SHAPE, where, "k and k_out go together")
-    if k is not None:
-        if k.dim() != 3:
-            _refuse(_SHAPE, where, f"k has to be [{tokens}, heads, {dim}], not {list(k.shape)}")
-        hk = k.shape[1]
-        sk, sko = _heads(where, "k", k, tokens, hk, dim, dtype, device), _heads(where, "k_out", k_out, tokens, hk, dim, dtype, device)
-    pos = _array(where, "positions", positions, (rope.num_axes, tokens), _torch.int32, device)
-    freq = _array(where, "inv_freq", inv_freq, (rope.rotary_dim // 2,), _torch.float32, device)
-    st = getattr(lib, where)(rope._ref, _code[dtype], q.data_ptr(), sq, k.data_ptr() if hk else None, sk, tokens, hq, hk, pos, freq,
-                             q_out.data_ptr(), sqo, k_out.data_ptr() if hk else None, sko, _stream(stream))
-    if st:
-        raise PrefixAttnError(st, where)
-
-
 def rope_axes_forward(rope: RopeAxes, q, k, positions, inv_freq, q_out, k_out, stream=None) -> None:
     """rope_axes_forward of the C ABI: the heads of q [T, Hq, D] and k [T, Hk, D] (or None, with k_out None) turned by positions
     [axes, T] int32 times inv_freq [rotary_dim / 2] fp32, into q_out and k_out (which may be q and k).  Heads are contiguous, tokens
     may be strided (slices of a fused projection).  Enqueues only."""
-    _rope_call("rope_axes_forward", rope, q, k, positions, inv_freq, q_out, k_out, stream)
+    _check("rope_axes_forward", (_native or _load_native()).rope(False, rope._address, q, k, positions, inv_freq, q_out, k_out, _stream(stream)))
 
 
 def rope_axes_backward(rope: RopeAxes, dq_out, dk_out, positions, inv_freq, dq, dk, stream=None) -> None:
     """rope_axes_backward of the C ABI: the gradients dq, dk of q and k from those of q_out and k_out, same shapes."""
-    _rope_call("rope_axes_backward", rope, dq_out, dk_out, positions, inv_freq, dq, dk, stream)
+    _check("rope_axes_backward", (_native or _load_native()).rope(True, rope._address, dq_out, dk_out, positions, inv_freq, dq, dk, _stream(stream)))
 
 
 class PagedAttnPlan:
@@ -239,59 +192,22 @@ def paged_attn_plan(num_q_heads: int, num_kv_heads: int, head_dim: int, page_siz
     st = lib.paged_attn_plan(ctypes.byref(d), ctypes.byref(h), ctypes.byref(ws))
     if st:
         raise PrefixAttnError(st, "paged_attn_plan")
-    kw.update(dtype=dtype, torch_dtype={"f32": _torch.float32, "bf16": _torch.bfloat16}[dtype],
-              cache_shape=(kw["num_pages"], kw["num_kv_heads"], kw["page_size"], kw["head_dim"]),
-              torch_device=_torch.device("cuda", kw["device"]) if device >= 0 else _torch.device("cpu"))
-    return PagedAttnPlan(h, ws.value, kw)
-
-
-def _call(where, plan, k_cache, v_cache, page_table, seq_lens, cu_new):
-    """Checks what every call on a plan takes; returns the pointers and the number of sequences."""
-    device, i32 = plan.torch_device, _torch.int32
-    seqs = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
-    return (_array(where, "k_cache", k_cache, plan.cache_shape, plan.torch_dtype, device),
-            _array(where, "v_cache", v_cache, plan.cache_shape, plan.torch_dtype, device),
-            _array(where, "page_table", page_table, (seqs, plan.max_pages_per_seq), i32, device),
-            _array(where, "seq_lens", seq_lens, (seqs,), i32, device),
-            _array(where, "cu_new", cu_new, (seqs + 1,), i32, device), seqs)
+    return PagedAttnPlan(h.value, ws.value, dict(kw, dtype=dtype))
 
 
 def paged_kv_append(plan: PagedAttnPlan, k, v, k_cache, v_cache, page_table, seq_lens, cu_new, stream=None) -> None:
     """paged_kv_append of the C ABI: the new tokens' k, v [T, Hkv, D] into their pages of the caches [num_pages, Hkv, page_size, D].
     page_table [B, max_pages_per_seq], seq_lens [B] (new tokens included) and cu_new [B + 1] (packed rows) are int32.  Enqueues only."""
-    where, lib = "paged_kv_append", _lib or _load()
-    kc, vc, table, lens, cu, seqs = _call(where, plan, k_cache, v_cache, page_table, seq_lens, cu_new)
-    tokens, hkv, dim = k.shape[0], plan.num_kv_heads, plan.head_dim
-    sk = _heads(where, "k", k, tokens, hkv, dim, plan.torch_dtype, plan.torch_device)
-    sv = _heads(where, "v", v, tokens, hkv, dim, plan.torch_dtype, plan.torch_device)
-    st = lib.paged_kv_append(plan.handle, k.data_ptr(), sk, v.data_ptr(), sv, kc, vc, table, lens, cu, seqs, tokens, _stream(stream))
-    if st:
-        raise PrefixAttnError(st, where)
+    _check("paged_kv_append", (_native or _load_native()).append(plan.handle, None, None, k, v, None, None, None, k_cache, v_cache, page_table,
+                                                                 seq_lens, cu_new, _stream(stream)))
 
 
 def paged_kv_append_rope(plan: PagedAttnPlan, rope: RopeAxes, q, k, v, positions, inv_freq, q_out, k_cache, v_cache, page_table,
                          seq_lens, cu_new, stream=None) -> None:
     """paged_kv_append_rope of the C ABI: the keys rotated as they are stored, and q [T, Hq, D] rotated into q_out (which may be q;
     both None to leave queries alone).  positions [axes, T] int32 and inv_freq as in rope_axes_forward.  Enqueues only."""
-    where, lib = "paged_kv_append_rope", _lib or _load()
-    kc, vc, table, lens, cu, seqs = _call(where, plan, k_cache, v_cache, page_table, seq_lens, cu_new)
-    tokens, hkv, dim, dtype, device = k.shape[0], plan.num_kv_heads, plan.head_dim, plan.torch_dtype, plan.torch_device
-    if rope.head_dim != dim:
-        _refuse(_SHAPE, where, f"the rotation is of heads of {rope.head_dim} channels, the plan's have {dim}")
-    sk, sv = _heads(where, "k", k, tokens, hkv, dim, dtype, device), _heads(where, "v", v, tokens, hkv, dim, dtype, device)
-    sq = sqo = 0
-    if (q is None) != (q_out is None):
-        _refuse(_SHAPE, where, "q and q_out go together")
-    if q is not None:
-        sq = _heads(where, "q", q, tokens, plan.num_q_heads, dim, dtype, device)
-        sqo = _heads(where, "q_out", q_out, tokens, plan.num_q_heads, dim, dtype, device)
-    pos = _array(where, "positions", positions, (rope.num_axes, tokens), _torch.int32, device)
-    freq = _array(where, "inv_freq", inv_freq, (rope.rotary_dim // 2,), _torch.float32, device)
-    st = lib.paged_kv_append_rope(plan.handle, rope._ref, None if q is None else q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv,
-                                  pos, freq, None if q is None else q_out.data_ptr(), sqo, kc, vc, table, lens, cu, seqs, tokens,
-                                  _stream(stream))
-    if st:
-        raise PrefixAttnError(st, where)
+    _check("paged_kv_append_rope", (_native or _load_native()).append(plan.handle, rope._address, q, k, v, positions, inv_freq, q_out, k_cache,
+                                                                      v_cache, page_table, seq_lens, cu_new, _stream(stream)))
 
 
 def paged_attn_forward(plan: PagedAttnPlan, q, k_cache, v_cache, page_table, seq_lens, cu_new, out, lse_out, workspace,
@@ -300,16 +216,5 @@ def paged_attn_forward(plan: PagedAttnPlan, q, k_cache, v_cache, page_table, seq
     [T, Hq, D] and lse_out [Hq, T] fp32 (or None).  The new tokens' keys and values are in the cache already (paged_kv_append).
     shared_len: None, or an int32 tensor of one element: so many leading tokens of all sequences are in the same pages, which
     calls of few rows then read once.  `workspace`: uint8, at least plan.workspace_bytes.  Enqueues only."""
-    where, lib = "paged_attn_forward", _lib or _load()
-    kc, vc, table, lens, cu, seqs = _call(where, plan, k_cache, v_cache, page_table, seq_lens, cu_new)
-    tokens, hq, dim, dtype, device = q.shape[0], plan.num_q_heads, plan.head_dim, plan.torch_dtype, plan.torch_device
-    sq = _heads(where, "q", q, tokens, hq, dim, dtype, device)
-    o = _array(where, "out", out, (tokens, hq, dim), dtype, device)
-    lse = None if lse_out is None else _array(where, "lse_out", lse_out, (hq, tokens), _torch.float32, device)
-    shared = None if shared_len is None else _array(where, "shared_len", shared_len, (1,), _torch.int32, device)
-    if workspace.device != device or not workspace.is_contiguous():
-        _refuse(_UNSUPPORTED, where, f"workspace has to be contiguous memory on {device}")
-    st = lib.paged_attn_forward(plan.handle, q.data_ptr(), sq, kc, vc, table, lens, cu, seqs, tokens, shared, o, lse,
-                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
-    if st:
-        raise PrefixAttnError(st, where)
+    _check("paged_attn_forward", (_native or _load_native()).attend(plan.handle, q, k_cache, v_cache, page_table, seq_lens, cu_new, out, lse_out,
+                                                                    workspace, shared_len, _stream(stream)))

@@ -52,12 +52,23 @@ def test_axes_of_pairs():
     assert pa.rope_axes((1, 3, 2), 16, rotary_dim=12, interleaved=True).pair_axis == (0, 1, 2, 1, 2, 1)
 
 
+def c_abi():
+    """The library's calls with the argument types of the header."""
+    lib = sampling._load()
+    i32, i64, vp, sz, rope = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.POINTER(sampling._RopeDesc)
+    call = [vp, vp, vp, i32, i64]            # page_table, seq_lens, cu_new, num_seqs, num_tokens
+    lib.rope_axes_forward.argtypes = [rope, i32, vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, i64, vp, i64, vp]
+    lib.paged_kv_append.argtypes = [vp, vp, i64, vp, i64, vp, vp, *call, vp]
+    lib.paged_kv_append_rope.argtypes = [vp, rope, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, *call, vp]
+    lib.paged_attn_forward.argtypes = [vp, vp, i64, vp, vp, *call, vp, vp, vp, vp, sz, vp]
+    return lib
+
+
 def raw(plan, call, **kw):
     """A call of the C ABI with plausible pointers; nothing of it is read, since every case is refused or the plan is host-only."""
-    lib = sampling._load()
-    p = 1 << 20
+    lib, p = c_abi(), 1 << 20
     a = dict(q=p, qs=28 * 128, k=p, ks=4 * 128, v=p, vs=4 * 128, pos=p, freq=p, qo=p, qos=28 * 128, kc=p, vc=p, table=p, lens=p, cu=p, seqs=4, tokens=4,
-             shared=None, out=p, lse=p, ws=p, bytes=1 << 40, rope=pa.rope_axes((64,), 128)._ref)
+             shared=None, out=p, lse=p, ws=p, bytes=1 << 40, rope=ctypes.byref(pa.rope_axes((64,), 128)._desc))
     a.update(kw)
     g = lambda names: [a[n] for n in names.split()]
     if call == "append":
@@ -84,7 +95,7 @@ def test_calls_check_their_arguments_before_launch():
         assert raw(h, "append", **{name: (1 << 20) + 1}) == 4
     assert raw(h, "rope", q=None) == 1 and raw(h, "rope", qo=None) == 1 and raw(h, "rope", q=None, qo=None) == 3
     assert raw(h, "rope", pos=None) == 1 and raw(h, "rope", freq=None) == 1 and raw(h, "rope", rope=None) == 1
-    assert raw(h, "rope", rope=pa.rope_axes((32,), 64)._ref) == 2 and raw(h, "rope", qs=28 * 128 - 1) == 2
+    assert raw(h, "rope", rope=ctypes.byref(pa.rope_axes((32,), 64)._desc)) == 2 and raw(h, "rope", qs=28 * 128 - 1) == 2
     for name in ("q", "out", "ws"):
         assert raw(h, "attend", **{name: None}) == 1 and raw(h, "attend", **{name: (1 << 20) + 8}) == 4
     assert raw(h, "attend", lse=None) == 3 and raw(h, "attend", lse=(1 << 20) + 2) == 4 and raw(h, "attend", shared=(1 << 20) + 2) == 4
@@ -96,7 +107,7 @@ def test_calls_check_their_arguments_before_launch():
 
 
 def test_rope_checks_its_arguments_before_launch():
-    lib, p = sampling._load(), 1 << 20
+    lib, p = c_abi(), 1 << 20
     desc = pa.rope_axes((20, 12), 64)._desc
 
     def call(d=desc, dtype=1, q=p, qs=256, k=p, ks=128, tokens=3, hq=4, hk=2, pos=p, freq=p, qo=p, qos=256, ko=p, kos=128):
@@ -141,7 +152,7 @@ def test_binding_refuses_tensors_that_do_not_fit():
     assert status(shared_len=torch.zeros(1)) == 3 and status(shared_len=torch.zeros(2, dtype=torch.int32)) == 2
     assert status(workspace=torch.empty(1, dtype=torch.uint8)) in (4, 5)
     with pytest.raises(pa.PrefixAttnError):
-        pa.paged_kv_append(plan, good["q"][:, :2], good["q"], *[good[n] for n in ("k_cache", "v_cache", "page_table", "seq_lens", "cu_new")])
+        pa.paged_kv_append(plan, good["q"][:, :2], good["q"], *[good[n] for n in ("k_cache", "v_cache", "page_table", "seq_lens", "cu_new")], stream=1)
     plan.destroy()
 
 
