@@ -30,6 +30,16 @@ def short_name(k: str) -> str:
         if sweep:
             return f"attention_{'ranges' if ranges else 'sweep'} (bf16 MFMA)" + (", fp32 partial" if epi == 0 else "")
         return "suffix_pass (bf16 MFMA)" + ("" if epi == 0 else ", final" if epi == 1 else ", merging")
+    if "paged_rows_kernel" in k:
+        return f"paged_attn_rows ({'fp32' if 'CoreF32' in k else 'bf16'} MFMA)"
+    if "paged_chunk_kernel" in k:
+        return "paged_attn_chunk (bf16 MFMA)"
+    if "merge_cuts_kernel" in k:
+        return "paged_attn: merge of cut blocks"
+    if "merge_rows_kernel" in k:
+        return "paged_attn: merge with shared keys"
+    if "rope_kernel" in k:      # <type, pairs are halves, into a paged cache>
+        return "paged_kv_append" if re.search(r"rope_kernel(I\w+?Lb\dELb1E|<.*, true>)", k) else "rope_axes"
     if "short_call_bf16_kernel" in k:   # whole calls of few key tiles, key ranges or whole blocks
         return "attention_short_call (bf16 MFMA)"
     if "bwd_dkv_reduce" in k:
