@@ -1,12 +1,14 @@
 // Attention of new tokens over their pages for chunks (bf16): blocks of 256 stacked rows.
 //
 // Bound: bf16 MFMA.  A block is 256 rows m = i * group + (h % group) of one kv head and sequence, 32 a wavefront, two wavefronts a SIMD;
-// tiles of 64 keys go to LDS once for all of them, two of K and two of V, one barrier a tile.  Products, operand order and the
+// tiles of 64 keys go to LDS once for all of them, three of K and of V (four at D = 64, where a tile's work is shorter than a load's
+// latency), one barrier a tile.  Products, operand order and the
 // interleave of one tile's softmax with the product before are those of the prefill kernels (v_mfma_f32_16x16x32_bf16 on transposed
 // scores); what differs:
 //   - Keys come from pages.  A wavefront loads 8 rows of a tile; they lie in one page (page sizes are multiples of 16), whose
 //     number is read into scalar registers one tile ahead, and the buffer descriptor is made for them: 64-bit address, range up to the
-//     last key, so that nothing past it is read and LDS holds zeros there.  Rows without a page become NaN keys.
+//     last key, so that nothing past it is read and LDS holds zeros there.  A row of the block that sees a key without a page, which is one
+//     whose limit is not below the smallest such key, becomes NaN at the end.
 //   - V is read transposed from row-major tiles (ds_read_b64_tr_b16): a paged cache has no images of its values.
 //   - The reference of the softmax is the maximum of a row's first tile, with no search afterwards; a tile's sum tells when some
 //     probability left the safe range.  Then the block is done again with its true maxima, which a pass over the
@@ -37,16 +39,16 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
   constexpr int LOADS = TILE_BYTES / 1024 / WAVES;  // 1 KiB loads of a wavefront, of K and of V
   constexpr int LANES_PER_ROW = ROWB / 16, ROWS_PER_LOAD = 1024 / ROWB;
   constexpr int WAVE_KEYS = TILE / WAVES;           // rows of a tile that a wavefront loads
-  constexpr int VBUF = 2 * TILE_BYTES;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_BYTES];
-  __shared__ int32_t gave_up[WAVES];
+  constexpr int AHEAD = 3, BUFS = AHEAD + 1;  // tiles under way beside the one that is read
+  constexpr int VBUF = BUFS * TILE_BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * BUFS * TILE_BYTES];
+  __shared__ int32_t gave_up[WAVES], wave_lost[WAVES];
 
   Walk walk;
   if (!begin_walk<THREADS>(a, walk)) return;
   const PagedShape& shape = walk.shape;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int page_mask = (1 << a.page_shift) - 1;
   const float c_log2 = a.scale * 1.4426950408889634f;
 
   int koff[KS], vtr[CB];
@@ -55,14 +57,14 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
     const int r = 4 * g4 + (l16 >> 2);
-    vtr[cb] = r * ROWB + (((2 * cb + ((l16 & 3) >> 1)) ^ swizzle_term_tr(r, ROWB)) << 4) + (l16 & 1) * 8;
+    vtr[cb] = r * ROWB + (((2 * cb + ((l16 & 3) >> 1)) ^ swizzle16(r, ROWB)) << 4) + (l16 & 1) * 8;
   }
   unsigned kload[LOADS], vload[LOADS];  // byte offset of this lane's 16 bytes in the wavefront's rows of the cache
 #pragma unroll
   for (int n = 0; n < LOADS; ++n) {
     const int in = n * ROWS_PER_LOAD + lane / LANES_PER_ROW, row = wave * WAVE_KEYS + in;
     kload[n] = (unsigned)(in * ROWB + (((lane % LANES_PER_ROW) ^ swizzle_term(row, ROWB)) << 4));
-    vload[n] = (unsigned)(in * ROWB + (((lane % LANES_PER_ROW) ^ swizzle_term_tr(row, ROWB)) << 4));
+    vload[n] = (unsigned)(in * ROWB + (((lane % LANES_PER_ROW) ^ swizzle16(row, ROWB)) << 4));
   }
 
   for (; walk.more(); walk.next(a)) {
@@ -91,34 +93,27 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
     // keys up to this one are seen by every row of the wavefront (positions do not fall from row to row)
     const int first_limit = __builtin_amdgcn_readfirstlane(limit[0]);
 
-    // The pages of a wavefront's rows of tile t: K's is looked up one tile before it is used, and V's is the same, one step later.
-    auto look_up = [&](int t) {
-      const int idx = (first_key + t * TILE + wave * WAVE_KEYS) >> a.page_shift;
-      const int page = read_const(table, idx < a.table_width ? idx : a.table_width - 1);
-      return idx < a.table_width && page >= 0 && page < a.num_pages ? page : -1;
+    // Where a wavefront's rows of tile t are: found for K, and used for V one step later.  The page number is read two steps before.
+    const uint32_t page_bytes = (uint32_t)((shape.Hkv << a.page_shift) * ROWB);
+    const int64_t head_bytes = ((int64_t)walk.head << a.page_shift) * ROWB;
+    const int wave_key = first_key + wave * WAVE_KEYS;
+    int last_key = first_key + tiles * TILE < p.key_end ? first_key + tiles * TILE : p.key_end;
+    int first_lost = last_key > shape.capacity ? shape.capacity : 0x7fffffff;  // smallest key without a page: rows that see it become NaN
+    last_key = last_key < shape.capacity ? last_key : shape.capacity;
+    auto look_up = [&](int t) { return page_of(a, table, wave_key + t * TILE); };
+    auto source = [&](int t, int page) {
+      return find_rows(a, page, page_bytes, head_bytes, wave_key + t * TILE, last_key, WAVE_KEYS, ROWB, first_lost);
     };
-    auto base_of = [&](int t, int page) -> int64_t {
-      const int key = first_key + t * TILE + wave * WAVE_KEYS;
-      return page < 0 ? 0 : ((((int64_t)page * shape.Hkv + walk.head) << a.page_shift) + (key & page_mask)) * ROWB;
-    };
-    auto bytes_of = [&](int t, int page) {
-      const int left = p.key_end - (first_key + t * TILE + wave * WAVE_KEYS);
-      return page < 0 || left <= 0 ? 0 : (left < WAVE_KEYS ? left : WAVE_KEYS) * ROWB;
-    };
-    auto issue_k = [&](int t, int page, auto buf_c) {
-      unsigned char* const dst = smem + decltype(buf_c)::value * TILE_BYTES + wave * LOADS * 1024;
-      if (page < 0 && first_key + t * TILE + wave * WAVE_KEYS < p.key_end) {
-#pragma unroll
-        for (int n = 0; n < LOADS; ++n) *reinterpret_cast<i32x4*>(dst + n * 1024 + lane * 16) = i32x4{0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0};
-        return;
-      }
-      const rsrc_t rs = make_rsrc(static_cast<const char*>(a.k_cache) + base_of(t, page), bytes_of(t, page));
+    // Every step issues as many loads as every other (empty ones behind the last tile), so that a wait can count them.
+    auto issue_k = [&](const Rows& from, int buf) {  // buf: byte offset of the buffer, K's and V's alike
+      unsigned char* const dst = smem + buf + wave * LOADS * 1024;
+      const rsrc_t rs = rows_rsrc(a.k_cache, from);
 #pragma unroll
       for (int n = 0; n < LOADS; ++n) load_chunk_to_lds(rs, dst + n * 1024, kload[n], 0);
     };
-    auto issue_v = [&](int t, int page, auto buf_c) {
-      unsigned char* const dst = smem + VBUF + decltype(buf_c)::value * TILE_BYTES + wave * LOADS * 1024;
-      const rsrc_t rs = make_rsrc(static_cast<const char*>(a.v_cache) + base_of(t, page), bytes_of(t, page));
+    auto issue_v = [&](const Rows& from, int buf) {
+      unsigned char* const dst = smem + VBUF + buf + wave * LOADS * 1024;
+      const rsrc_t rs = rows_rsrc(a.v_cache, from);
 #pragma unroll
       for (int n = 0; n < LOADS; ++n) load_chunk_to_lds(rs, dst + n * 1024, vload[n], 0);
     };
@@ -129,7 +124,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
     float mref[NQ], lsum[NQ];
     bool bad = false;
 
-    auto scores = [&](const unsigned char* kbuf, auto&& mid) {
+    auto scores = [&](const unsigned char* kbuf) {
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
@@ -147,7 +142,6 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
         for (int nq = 0; nq < NQ; ++nq)
           S[t % 4][nq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[t % RING], Q[nq][t / 4], S[t % 4][nq], 0, 0, 0);
         if (t + RING < OPS) ka[t % RING] = operand(t + RING);
-        mid(t);
         __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
@@ -227,8 +221,6 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
       __builtin_amdgcn_s_setprio(0);
     };
 
-    using B0 = std::integral_constant<int, 0>;
-    using B1 = std::integral_constant<int, 1>;
     // Once; and, where some row's probabilities left the safe range, once more with the true maxima.
     for (int again = 0; tiles > 0; ++again) {
 #pragma unroll
@@ -241,23 +233,29 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
       bad = false;
       if (again) {
         for (int t = 0; t < tiles; ++t) {
-          issue_k(t, look_up(t), B0{});
+          issue_k(source(t, look_up(t)), 0);
           wait_loads<0>();
           __syncthreads();
-          scores(smem, [](int) {});
+          scores(smem);
           mask(t);
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq) mref[nq] = fmaxf(mref[nq], row_max(nq));
           __syncthreads();
         }
       }
-      int page = look_up(0), page1 = look_up(1);  // of the tile whose V comes next, and of the tile whose K does
-      issue_k(0, page, B0{});
-      issue_v(0, page, B0{});
-      if (tiles > 1) issue_k(1, page1, B1{});
-      wait_loads<0>();
+      Rows from = source(0, look_up(0));  // of the last tile whose K was issued
+      issue_k(from, 0);
+      auto issue_next = [&](int t, int page, int vbuf, int kbuf) {  // V of tile t - 1 and K of tile t
+        issue_v(from, vbuf);
+        from = source(t, page);
+        issue_k(from, kbuf);
+      };
+#pragma unroll
+      for (int t = 1; t <= AHEAD; ++t) issue_next(t, look_up(t), (t - 1) * TILE_BYTES, t * TILE_BYTES);
+      int page = look_up(AHEAD + 1);
+      wait_loads<AHEAD * 2 * LOADS>();  // K of tile 0
       __syncthreads();
-      scores(smem, [](int) {});
+      scores(smem);
       mask(0);
       {
         bf16x8 Pn[2][NQ];
@@ -275,36 +273,33 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
         for (int j = 0; j < 4 * NQ; ++j) slice(j, mc, Pn, lacc);
         accept(Pn, lacc);
       }
+      wait_loads<(AHEAD - 1) * 2 * LOADS>();
       __syncthreads();
-      auto step = [&](int t, auto buf_c) {
-        constexpr int BUF = decltype(buf_c)::value;
-        const int page2 = look_up(t + 1);
-        scores(smem + BUF * TILE_BYTES, [&](int o) {
-          if (o == 1 && t + 1 < tiles) issue_k(t + 1, page2, std::integral_constant<int, BUF ^ 1>{});
-          if (o == 2 * KS + 1) issue_v(t, page1, buf_c);
-        });
-        page1 = page2;
+      // Step t: the scores of tile t, then the product of tile t - 1 and the softmax of tile t.  Tile t is in buffer t % BUFS; K of
+      // tile t + AHEAD goes where K of tile t - 1 was, V of the tile before it where V of tile t - 2 was.
+      int buf = 0;  // of tile t - 1
+      for (int t = 1; t < tiles; ++t) {
+        const int old = buf, older = old == 0 ? AHEAD * TILE_BYTES : old - TILE_BYTES;
+        buf = old == AHEAD * TILE_BYTES ? 0 : old + TILE_BYTES;
+        scores(smem + buf);
         mask(t);
         bf16x8 Pn[2][NQ];
         float lacc[NQ];
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) lacc[nq] = 0.f;
-        product(smem + VBUF + (BUF ^ 1) * TILE_BYTES, std::true_type{}, Pn, lacc);
+        product(smem + VBUF + old, std::true_type{}, Pn, lacc);
         accept(Pn, lacc);
-        wait_loads<0>();
+        issue_next(t + AHEAD, page, older, old);
+        page = look_up(t + AHEAD + 1);
+        wait_loads<(AHEAD - 1) * 2 * LOADS>();  // K of tile t + 1 and V of tile t
         __syncthreads();
-      };
-      int t = 1;
-      for (; t + 1 < tiles; t += 2) {
-        step(t, B1{});
-        step(t + 1, B0{});
       }
-      if (t < tiles) step(t, B1{});
       {
         bf16x8 Pn[2][NQ];
         float lacc[NQ];
-        product(smem + VBUF + ((tiles - 1) & 1) * TILE_BYTES, std::false_type{}, Pn, lacc);
+        product(smem + VBUF + buf, std::false_type{}, Pn, lacc);
       }
+      wait_loads<0>();  // the empty ones too: the next loads go over their places
       if (again) break;
       if (lane == 0) gave_up[wave] = bad ? 1 : 0;
       __syncthreads();
@@ -314,18 +309,30 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
       if (__builtin_amdgcn_readfirstlane(any) == 0) break;
       __syncthreads();
     }
+    if (lane == 0) wave_lost[wave] = first_lost;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) first_lost = wave_lost[w] < first_lost ? wave_lost[w] : first_lost;
 
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
       const int r = wave * ROWS_PER_WAVE + nq * 16 + l16;
-      const float l = tiles > 0 ? quad_sum(lsum[nq]) : 0.f;
+      float l = tiles > 0 ? quad_sum(lsum[nq]) : 0.f;
+      if (r >= block_rows) continue;
+      if (limit[nq] >= first_lost) l = NAN;
       const float inv = l == 0.f ? 0.f : 1.f / l;  // 0: no key is seen
-      if (r < block_rows) {
-        const Place dst = walk.place(a, p, r);
+      const float lse = tiles > 0 ? mref[nq] * a.scale + __logf(l) : -INFINITY;
+      const Place dst = walk.place(a, p, r);
+      auto value = [&](int cb) { return tiles > 0 ? O[cb][nq] * inv : f32x4{0.f, 0.f, 0.f, 0.f}; };
+      if (dst.partial) {
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) write_row<__bf16>(dst, 16 * cb + 4 * g4, tiles > 0 ? O[cb][nq] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
-        if (g4 == 0 && dst.lse) *dst.lse = tiles > 0 ? mref[nq] * a.scale + __logf(l) : -INFINITY;
+        for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<f32x4*>(static_cast<float*>(dst.row) + 16 * cb + 4 * g4) = value(cb);
+      } else {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+          *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(dst.row) + 16 * cb + 4 * g4) = __builtin_convertvector(value(cb), bf16x4);
       }
+      if (g4 == 0 && dst.lse) *dst.lse = lse;
     }
     walk.note_cut(a);
     __syncthreads();  // all reads of the tiles are over before the next block's loads come

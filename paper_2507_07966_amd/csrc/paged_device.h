@@ -27,6 +27,14 @@ __device__ inline float quad_sum(float x) {
   return a + b;
 }
 
+// Swizzle of row-major tiles that are read both as 16-byte operands (16 consecutive rows at one 16-byte chunk) and transposed in 16 x 16
+// blocks (ds_read_b64_tr_b16: lane l of a group of 16 reads 8 bytes of row 4 g + l / 4, so half a wavefront reads 32 bytes of 8
+// consecutive rows): chunk c of row r is stored at c ^ swizzle16(r), which puts the pieces of either access on different banks.
+__device__ inline int swizzle16(int row, int row_bytes) {
+  const int low = ((row >> 1) & 2) | ((row >> 3) & 1);
+  return row_bytes == 256 ? ((row & 3) << 2) | low : ((row & 2) << 1) | low;
+}
+
 // Wait until at most N of this wavefront's vector memory operations are under way (loads to LDS complete in order), or until its
 // reads of LDS have returned.  The compiler keeps memory accesses on their side of it.
 template <int N>
@@ -71,6 +79,34 @@ __device__ inline Segment load_segment(const PagedArgs& a, const PagedShape& s, 
 __device__ inline int32_t row_limit(const PagedShape& s, const Segment& g, int32_t token) {
   const int32_t pos = g.first_pos + token;
   return pos < 0 ? -1 : pos < s.capacity ? pos : s.capacity;
+}
+
+// Where some consecutive rows of a head are in the cache.  They lie in one page; the buffer descriptor's range ends with the last row that
+// exists, or is empty, and LDS receives zeros behind it.
+struct Rows {
+  int64_t off;  // bytes from the cache's begin
+  int32_t bytes;
+};
+// `key`: the first of `count` rows of `row_bytes`; keys from `end` on do not exist.  `first_lost` becomes the smallest key without a page.
+__device__ inline Rows find_rows(const PagedArgs& a, int32_t page, uint32_t page_bytes, int64_t head_bytes, int32_t key, int32_t end,
+                                 int32_t count, int32_t row_bytes, int32_t& first_lost) {
+  const int32_t left = end - key < count ? end - key : count;
+  const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
+  if (!ok && left > 0) first_lost = key < first_lost ? key : first_lost;
+  return Rows{(int64_t)((uint64_t)(uint32_t)page * page_bytes) + head_bytes + (key & ((1 << a.page_shift) - 1)) * row_bytes,
+              ok && left > 0 ? left * row_bytes : 0};
+}
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ inline mt::rsrc_t rows_rsrc(const void* cache, const Rows& r) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(cache) + r.off), 0, r.bytes, 0x00020000);
+}
+#else
+__device__ inline mt::rsrc_t rows_rsrc(const void*, const Rows&) { return {}; }
+#endif
+// The page of `key` in a row of the page table (keys behind the table: of its last column, they do not exist)
+__device__ inline int32_t page_of(const PagedArgs& a, const int32_t* table, int32_t key) {
+  const int32_t idx = key >> a.page_shift;
+  return read_const(table, idx < a.table_width ? idx : a.table_width - 1);
 }
 
 // A workgroup's way along its share: one piece of a block at a time.  All members are uniform.

@@ -9,7 +9,8 @@
 //     loads (STAGES of them in flight or in use: 128 KiB a compute unit, which covers latency times rate), and
 //     waits for its own loads only; there is no barrier inside a block.  A page is looked up once for 16 keys (page
 //     sizes are multiples of 16), in scalar registers one stage ahead; the loads' range ends at the last key or is empty where a page
-//     is missing, so LDS holds zeros there and nothing outside the cache is read.
+//     is missing, so LDS holds zeros there and nothing outside the cache is read.  A row that sees a key without a page, which is one whose
+//     limit is not below the smallest such key, becomes NaN at the end.
 //   - Scores are formed transposed, S^T = K Q^T, so that a lane holds scores of one query and the probabilities are the operand of
 //     O^T += V^T P^T as they are.  bf16: v_mfma_f32_16x16x32_bf16, V read transposed from LDS (ds_read_b64_tr_b16).
 //     fp32: v_mfma_f32_16x16x4_f32; channels are dealt to the steps of the product such that every LDS read is 16 bytes a
@@ -42,7 +43,7 @@ struct CoreBf16 {
   bf16x8 Q[NQ][KS];
   f32x4 O[CB][NQ];
   int koff[KS], vtr[CB];
-  __device__ static int swizzle(int row) { return swizzle_term_tr(row, ROWB); }
+  __device__ static int swizzle(int row) { return swizzle16(row, ROWB); }
   __device__ void init(int l16, int g4) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) koff[ks] = l16 * ROWB + (((4 * ks + g4) ^ swizzle(l16)) << 4);
@@ -193,7 +194,6 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
   const PagedShape& shape = walk.shape;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int page_mask = (1 << a.page_shift) - 1;
   const float c_log2 = a.scale * 1.4426950408889634f;
 
   Core core;
@@ -218,32 +218,23 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
     const int stages = span > 0 ? (span + WAVES * KEYS - 1) / (WAVES * KEYS) : 0;
     const int key_base = first_key + wave * KEYS;
 
+    const uint32_t page_bytes = (uint32_t)((shape.Hkv << a.page_shift) * ROWB);
+    const int64_t head_bytes = ((int64_t)walk.head << a.page_shift) * ROWB;
+    int first_lost = last_key > shape.capacity ? shape.capacity : 0x7fffffff;  // smallest key without a page: rows that see it become NaN
+    const int end = last_key < shape.capacity ? last_key : shape.capacity;
     int pid[KB];  // pages of the next stage to be loaded
     auto look_up = [&](int s) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const int idx = (key_base + s * WAVES * KEYS + 16 * kb) >> a.page_shift;
-        pid[kb] = read_const(table, idx < a.table_width ? idx : a.table_width - 1);
-      }
+      for (int kb = 0; kb < KB; ++kb) pid[kb] = page_of(a, table, key_base + s * WAVES * KEYS + 16 * kb);
     };
     using B0 = std::integral_constant<int, 0>;
     using B1 = std::integral_constant<int, 1>;
-    int lost[STAGES];  // bit kb: the 16 keys have no page
     auto load = [&](int s, auto buf_c) {
-      constexpr int BUF = decltype(buf_c)::value;
-      unsigned char* const dst = my_ring + BUF * 2 * HALF_STAGE;
-      lost[BUF] = 0;
+      unsigned char* const dst = my_ring + decltype(buf_c)::value * 2 * HALF_STAGE;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        const int key = key_base + s * WAVES * KEYS + 16 * kb;
-        const int64_t page = pid[kb];
-        const bool ok = page >= 0 && page < a.num_pages && key >> a.page_shift < a.table_width;
-        const int left = last_key - key;
-        const int bytes = !ok || left <= 0 ? 0 : (left < 16 ? left : 16) * ROWB;
-        if (!ok && left > 0) lost[BUF] |= 1 << kb;
-        const int64_t off = ok ? ((((page * shape.Hkv + walk.head) << a.page_shift) + (key & page_mask)) * ROWB) : 0;
-        const rsrc_t kr = make_rsrc(static_cast<const char*>(a.k_cache) + off, bytes);
-        const rsrc_t vr = make_rsrc(static_cast<const char*>(a.v_cache) + off, bytes);
+        const Rows from = find_rows(a, pid[kb], page_bytes, head_bytes, key_base + s * WAVES * KEYS + 16 * kb, end, 16, ROWB, first_lost);
+        const rsrc_t kr = rows_rsrc(a.k_cache, from), vr = rows_rsrc(a.v_cache, from);
 #pragma unroll
         for (int n = 0; n < GROUP_LOADS; ++n) load_chunk_to_lds(kr, dst + kb * 16 * ROWB + n * 1024, loff[n], 0);
 #pragma unroll
@@ -252,7 +243,6 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
     };
 
     look_up(0);
-
     int limit[NQ];  // last key that query column nq sees
     int least = 0x7fffffff;
 #pragma unroll
@@ -263,7 +253,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       if (r < block_rows) {
         const int tok = walk.row_token(r);
         row = static_cast<const T*>(a.q) + (int64_t)(seg.token0 + tok) * a.q_stride + walk.row_head(r, tok) * D;
-        if (!walk.shared) limit[nq] = row_limit(shape, seg, tok);
+        limit[nq] = walk.shared ? p.key_end - 1 : row_limit(shape, seg, tok);
       }
       core.load_q(nq, row, g4);
       least = limit[nq] < least ? limit[nq] : least;
@@ -289,12 +279,12 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       for (int cb = 0; cb < CB; ++cb) core.O[cb][nq] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    auto compute = [&](int s, int lost_now) {
+    auto compute = [&](int s) {
       f32x4 S[KB][NQ];
       core.scores(S);
       const int key0 = key_base + s * WAVES * KEYS;
       const int seen = first_limit < last_key - 1 ? first_limit : last_key - 1;
-      if (key0 + KEYS - 1 > seen || lost_now) {
+      if (key0 + KEYS - 1 > seen) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -303,7 +293,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int key = key0 + 16 * kb + 4 * g4 + i;
-              S[kb][nq][i] = key > last ? -INFINITY : (lost_now >> kb) & 1 ? NAN : S[kb][nq][i];
+              if (key > last) S[kb][nq][i] = -INFINITY;
             }
           }
       }
@@ -346,13 +336,12 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       // this stage's loads are done when at most those of the next one are under way
       if (s + 1 < stages) wait_loads<LOADS>(); else wait_loads<0>();
       core.read(kbuf, kbuf + HALF_STAGE);
-      const int lost_now = lost[BUF];
       if (s + 2 < stages) {  // all operands are in registers: the loads of the stage after the next one go over them
         wait_lds_reads();
         load(s + 2, buf_c);
         if (s + 3 < stages) look_up(s + 3);
       }
-      compute(s, lost_now);
+      compute(s);
     };
     for (int s = 0; s < stages; s += 2) {
       step(s, B0{});
@@ -363,7 +352,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
     //      at chunk c ^ (r & 15): rows written by 16 lanes at one chunk fall on all banks)
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
-      const float l = quad_sum(sum[nq]);
+      const float l = limit[nq] >= first_lost ? NAN : quad_sum(sum[nq]);
       if (g4 == 0) {
         wave_max[wave][nq * 16 + l16] = top[nq];
         wave_sum[wave][nq * 16 + l16] = l;
