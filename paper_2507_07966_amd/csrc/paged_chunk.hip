@@ -107,15 +107,13 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
     // Every step issues as many loads as every other (empty ones behind the last tile), so that a wait can count them.
     auto issue_k = [&](const Rows& from, int buf) {  // buf: byte offset of the buffer, K's and V's alike
       unsigned char* const dst = smem + buf + wave * LOADS * 1024;
-      const rsrc_t rs = rows_rsrc(a.k_cache, from);
 #pragma unroll
-      for (int n = 0; n < LOADS; ++n) load_chunk_to_lds(rs, dst + n * 1024, kload[n], 0);
+      for (int n = 0; n < LOADS; ++n) load_chunk_to_lds_uncounted(a.k_cache, from, dst + n * 1024, kload[n]);
     };
     auto issue_v = [&](const Rows& from, int buf) {
       unsigned char* const dst = smem + VBUF + buf + wave * LOADS * 1024;
-      const rsrc_t rs = rows_rsrc(a.v_cache, from);
 #pragma unroll
-      for (int n = 0; n < LOADS; ++n) load_chunk_to_lds(rs, dst + n * 1024, vload[n], 0);
+      for (int n = 0; n < LOADS; ++n) load_chunk_to_lds_uncounted(a.v_cache, from, dst + n * 1024, vload[n]);
     };
 
     f32x4 O[CB][NQ];    // O^T: register i of block cb is channel 16 cb + 4 g4 + i of column nq
@@ -254,7 +252,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
       for (int t = 1; t <= AHEAD; ++t) issue_next(t, look_up(t), (t - 1) * TILE_BYTES, t * TILE_BYTES);
       int page = look_up(AHEAD + 1);
       wait_loads<AHEAD * 2 * LOADS>();  // K of tile 0
-      __syncthreads();
+      barrier_with_loads();
       scores(smem);
       mask(0);
       {
@@ -274,7 +272,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
         accept(Pn, lacc);
       }
       wait_loads<(AHEAD - 1) * 2 * LOADS>();
-      __syncthreads();
+      barrier_with_loads();
       // Step t: the scores of tile t, then the product of tile t - 1 and the softmax of tile t.  Tile t is in buffer t % BUFS; K of
       // tile t + AHEAD goes where K of tile t - 1 was, V of the tile before it where V of tile t - 2 was.
       int buf = 0;  // of tile t - 1
@@ -292,7 +290,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
         issue_next(t + AHEAD, page, older, old);
         page = look_up(t + AHEAD + 1);
         wait_loads<(AHEAD - 1) * 2 * LOADS>();  // K of tile t + 1 and V of tile t
-        __syncthreads();
+        barrier_with_loads();
       }
       {
         bf16x8 Pn[2][NQ];

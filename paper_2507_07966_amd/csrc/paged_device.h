@@ -41,6 +41,12 @@ template <int N>
 __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// A barrier that does not wait for loads to LDS, as __syncthreads() does: the caller has waited for those that the workgroup is to see.
+__device__ inline void barrier_with_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 __device__ inline void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Lengths, tables and the like: nothing writes them while a kernel runs, which the address space says, so that uniform reads are scalar.
@@ -95,6 +101,19 @@ __device__ inline Rows find_rows(const PagedArgs& a, int32_t page, uint32_t page
   if (!ok && left > 0) first_lost = key < first_lost ? key : first_lost;
   return Rows{(int64_t)((uint64_t)(uint32_t)page * page_bytes) + head_bytes + (key & ((1 << a.page_shift) - 1)) * row_bytes,
               ok && left > 0 ? left * row_bytes : 0};
+}
+// 16 bytes a lane straight to LDS (lane l's land at dst + 16 l) that the compiler does not know of.  It waits for every load to LDS that it
+// knows of before the next read of LDS that may overlap it, and it cannot tell the buffers of a ring apart: a kernel that has later tiles
+// under way while it reads an earlier one counts its loads itself (wait_loads).  s_nop 4: a descriptor that a vector instruction
+// has just written to scalar registers may be read by a buffer instruction five states later, m0 one.
+__device__ inline void load_chunk_to_lds_uncounted(const void* cache, const Rows& r, unsigned char* dst, unsigned lane_byte_offset) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint64_t base = (uint64_t)(uintptr_t)cache + (uint64_t)r.off;
+  const mt::i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff),
+                          __builtin_amdgcn_readfirstlane(r.bytes), 0x00020000};
+  const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(PA_LDS_PTR(unsigned char))dst);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(lane_byte_offset), "s"(rsrc) : "memory", "m0");
+#endif
 }
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ inline mt::rsrc_t rows_rsrc(const void* cache, const Rows& r) {
