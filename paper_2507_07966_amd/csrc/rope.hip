@@ -5,9 +5,10 @@
 //
 // Mapping: a head's channels are split into units of W channel pairs (16 bytes of each of the two channels of a pair, or of W / 2
 // neighbouring pairs), of W channels that pass through, and of single pairs and channels where a size is no multiple of W.
-// A thread owns one unit of one token, forms the unit's sines and cosines once in registers, and turns that unit of several
-// heads (HPT of them in large calls, one in small ones, where latency counts).  Vector accesses are declared with the alignment
-// of an element, so slices at any offset take the same path.
+// A thread owns one unit of one token, forms the unit's sines and cosines once in registers, and turns that unit of HPT heads: four or
+// eight in large calls, one in small ones, where latency counts.  The heads' loads are issued before the sines are worked out
+// (32,768 tokens, 28 + 4 heads of 128, bf16: 132 -> 111 us, 4.8 TB/s).  Large calls store past the caches (139 -> 132 us before that;
+// appended chunks, whose values are only copied, 50 -> 37 us).  Vector accesses are declared with the alignment of an element, so slices at any offset take the same path.
 #include <hip/hip_runtime.h>
 
 #include "common.h"
@@ -17,7 +18,6 @@ namespace pa {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int MAX_HPT = 4;  // heads whose loads a thread has in flight at once
 
 // cos and sin of `pos * inv_freq`: the angle in quarter turns is formed and reduced in 64 bits (a position of 2^31 leaves an
 // error of 2e-7 quarter turns), the remainder |x| <= pi / 4 goes through the Taylor series, whose first left-out
@@ -64,14 +64,19 @@ struct Units {
 
 struct RopeKernelArgs {
   RopeArgs a;
-  int heads_per_group;  // groups of heads that a token is split over: thread (token, group g, unit) does heads g, g + groups, ...
-  int tokens;           // per workgroup
-  int groups;
+  int tokens;  // per workgroup
+  int groups;  // of heads that a token is split over: thread (token, group g, unit) does heads g, g + groups, ...
 };
 
-template <typename T, bool HALVES, bool APPEND>
+template <bool PAST_CACHES, typename V, typename VU>
+__device__ inline void store(VU* p, V x) {
+  if (PAST_CACHES) __builtin_nontemporal_store(x, p); else *p = x;
+}
+
+template <typename T, bool HALVES, bool APPEND, int HPT>
 __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) {
   constexpr int W = 16 / sizeof(T);
+  constexpr bool LARGE = HPT > 1;
   using V = typename Vec<T, W>::type;
   using VU = typename Vec<T, W>::unaligned;
   const RopeArgs& a = ka.a;
@@ -132,6 +137,40 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) 
       kind = PASS_ONE;
       ca = cb = R + units.pass * W + (u - units.pass);
     }
+    const T* src[HPT];
+    T* dst[HPT];
+    bool turn[HPT];
+    V xa[HPT], xb[HPT];
+#pragma unroll
+    for (int i = 0; i < HPT; ++i) {
+      const int h = g + i * ka.groups;
+      src[i] = nullptr;
+      turn[i] = true;
+      if (h < a.Hq) {
+        src[i] = static_cast<const T*>(a.q) + t * a.q_stride + h * D;
+        dst[i] = static_cast<T*>(a.q_out) + t * a.q_out_stride + h * D;
+      } else if (h < a.Hq + a.Hk) {
+        const int hk = h - a.Hq;
+        src[i] = static_cast<const T*>(a.k) + t * a.k_stride + hk * D;
+        dst[i] = APPEND ? static_cast<T*>(a.k_cache) + (at + ((int64_t)hk << a.page_shift)) * D
+                        : static_cast<T*>(a.k_out) + t * a.k_out_stride + hk * D;
+        if (APPEND && at < 0) src[i] = nullptr;
+      } else if (APPEND && h < heads) {
+        const int hv = h - a.Hq - a.Hk;
+        src[i] = static_cast<const T*>(a.v) + t * a.v_stride + hv * D;
+        dst[i] = static_cast<T*>(a.v_cache) + (at + ((int64_t)hv << a.page_shift)) * D;
+        turn[i] = false;
+        if (at < 0) src[i] = nullptr;
+      }
+      if (!src[i]) continue;
+      if (kind == TURN || kind == PASS) {
+        xa[i] = *reinterpret_cast<const VU*>(src[i] + ca);
+        if (HALVES && kind == TURN) xb[i] = *reinterpret_cast<const VU*>(src[i] + cb);
+      } else {
+        xa[i][0] = src[i][ca];
+        if (kind == TURN_ONE) xb[i][0] = src[i][cb];
+      }
+    }
     constexpr int N = HALVES ? W : W / 2;  // pairs of a full unit
     float cs[N], sn[N];
     if (kind == TURN || kind == TURN_ONE) {
@@ -147,73 +186,37 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) 
         }
       }
     }
-    for (int h0 = g; h0 < heads; h0 += ka.groups * MAX_HPT) {
-      const T* src[MAX_HPT];
-      T* dst[MAX_HPT];
-      bool turn[MAX_HPT];
-      V xa[MAX_HPT], xb[MAX_HPT];
 #pragma unroll
-      for (int i = 0; i < MAX_HPT; ++i) {
-        const int h = h0 + i * ka.groups;
-        src[i] = nullptr;
-        turn[i] = true;
-        if (h < a.Hq) {
-          src[i] = static_cast<const T*>(a.q) + t * a.q_stride + h * D;
-          dst[i] = static_cast<T*>(a.q_out) + t * a.q_out_stride + h * D;
-        } else if (h < a.Hq + a.Hk) {
-          const int hk = h - a.Hq;
-          src[i] = static_cast<const T*>(a.k) + t * a.k_stride + hk * D;
-          dst[i] = APPEND ? static_cast<T*>(a.k_cache) + (at + ((int64_t)hk << a.page_shift)) * D
-                          : static_cast<T*>(a.k_out) + t * a.k_out_stride + hk * D;
-          if (APPEND && at < 0) src[i] = nullptr;
-        } else if (APPEND && h < heads) {
-          const int hv = h - a.Hq - a.Hk;
-          src[i] = static_cast<const T*>(a.v) + t * a.v_stride + hv * D;
-          dst[i] = static_cast<T*>(a.v_cache) + (at + ((int64_t)hv << a.page_shift)) * D;
-          turn[i] = false;
-          if (at < 0) src[i] = nullptr;
-        }
-        if (!src[i]) continue;
-        if (kind == TURN || kind == PASS) {
-          xa[i] = *reinterpret_cast<const VU*>(src[i] + ca);
-          if (HALVES && kind == TURN) xb[i] = *reinterpret_cast<const VU*>(src[i] + cb);
-        } else {
-          xa[i][0] = src[i][ca];
-          if (kind == TURN_ONE) xb[i][0] = src[i][cb];
-        }
-      }
+    for (int i = 0; i < HPT; ++i) {
+      if (!src[i]) continue;
+      T* y = dst[i];
+      if (kind == PASS || (kind == TURN && !turn[i])) {
+        store<LARGE>(reinterpret_cast<VU*>(y + ca), xa[i]);
+        if (HALVES && kind == TURN) store<LARGE>(reinterpret_cast<VU*>(y + cb), xb[i]);
+      } else if (kind == PASS_ONE || !turn[i]) {
+        y[ca] = xa[i][0];
+        if (kind == TURN_ONE) y[cb] = xb[i][0];
+      } else if (kind == TURN) {
+        V ya, yb;
 #pragma unroll
-      for (int i = 0; i < MAX_HPT; ++i) {
-        if (!src[i]) continue;
-        T* y = dst[i];
-        if (kind == PASS || (kind == TURN && !turn[i])) {
-          *reinterpret_cast<VU*>(y + ca) = xa[i];
-          if (HALVES && kind == TURN) *reinterpret_cast<VU*>(y + cb) = xb[i];
-        } else if (kind == PASS_ONE || !turn[i]) {
-          y[ca] = xa[i][0];
-          if (kind == TURN_ONE) y[cb] = xb[i][0];
-        } else if (kind == TURN) {
-          V ya, yb;
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const float x0 = HALVES ? (float)xa[i][e] : (float)xa[i][2 * e % W];
-            const float x1 = HALVES ? (float)xb[i][e] : (float)xa[i][(2 * e + 1) % W];
-            const float y0 = x0 * cs[e] - x1 * sn[e], y1 = x1 * cs[e] + x0 * sn[e];  // rounded to T once
-            if (HALVES) {
-              ya[e] = (T)y0;
-              yb[e] = (T)y1;
-            } else {
-              ya[2 * e % W] = (T)y0;
-              ya[(2 * e + 1) % W] = (T)y1;
-            }
+        for (int e = 0; e < N; ++e) {
+          const float x0 = HALVES ? (float)xa[i][e] : (float)xa[i][2 * e % W];
+          const float x1 = HALVES ? (float)xb[i][e] : (float)xa[i][(2 * e + 1) % W];
+          const float y0 = x0 * cs[e] - x1 * sn[e], y1 = x1 * cs[e] + x0 * sn[e];  // rounded to T once
+          if (HALVES) {
+            ya[e] = (T)y0;
+            yb[e] = (T)y1;
+          } else {
+            ya[2 * e % W] = (T)y0;
+            ya[(2 * e + 1) % W] = (T)y1;
           }
-          *reinterpret_cast<VU*>(y + ca) = ya;
-          if (HALVES) *reinterpret_cast<VU*>(y + cb) = yb;
-        } else {
-          const float x0 = (float)xa[i][0], x1 = (float)xb[i][0];
-          y[ca] = (T)(x0 * cs[0] - x1 * sn[0]);
-          y[cb] = (T)(x1 * cs[0] + x0 * sn[0]);
         }
+        store<LARGE>(reinterpret_cast<VU*>(y + ca), ya);
+        if (HALVES) store<LARGE>(reinterpret_cast<VU*>(y + cb), yb);
+      } else {
+        const float x0 = (float)xa[i][0], x1 = (float)xb[i][0];
+        y[ca] = (T)(x0 * cs[0] - x1 * sn[0]);
+        y[cb] = (T)(x1 * cs[0] + x0 * sn[0]);
       }
     }
   }
@@ -225,15 +228,20 @@ int launch(const RopeArgs& a, void* stream) {
   const int heads = a.Hq + a.Hk + a.Hv;
   RopeKernelArgs k;
   k.a = a;
-  // One head to a thread while the call cannot fill the chip with wavefronts; then MAX_HPT heads share the sines.
-  const int hpt = a.T * heads * units.count() < (int64_t)NUM_CU * THREADS * MAX_HPT ? 1 : MAX_HPT;
+  // As many heads as leave a few wavefronts to every SIMD: 8 from 2^21 units on (2^18 threads), 4 from 2^18 on.  In fp32, 5,377 tokens, 14 +
+  // 2 heads of 64 (2^20.6 units): 12.7 us with 4, 14.0 with 8; bf16, 18,432 tokens, 28 + 4 of 128 (2^22.2): 68.6 and 61.3.
+  const int64_t work = a.T * heads * units.count();
+  const int hpt = work >= (1 << 21) ? 8 : work >= (1 << 18) ? 4 : 1;
   k.groups = (heads + hpt - 1) / hpt;
   const int per_token = units.count() * k.groups;
   k.tokens = per_token >= THREADS ? 1 : THREADS / per_token;
   const int64_t blocks = (a.T + k.tokens - 1) / k.tokens;
   const unsigned gx = (unsigned)(blocks < MAX_GRID_X ? blocks : MAX_GRID_X);
   const unsigned gy = (unsigned)((blocks + gx - 1) / gx);
-  rope_kernel<T, HALVES, APPEND><<<dim3(gx, gy), THREADS, 0, static_cast<hipStream_t>(stream)>>>(k);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (hpt == 8) rope_kernel<T, HALVES, APPEND, 8><<<dim3(gx, gy), THREADS, 0, st>>>(k);
+  else if (hpt == 4) rope_kernel<T, HALVES, APPEND, 4><<<dim3(gx, gy), THREADS, 0, st>>>(k);
+  else rope_kernel<T, HALVES, APPEND, 1><<<dim3(gx, gy), THREADS, 0, st>>>(k);
   return (int)hipGetLastError();
 }
 

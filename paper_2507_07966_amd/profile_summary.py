@@ -38,8 +38,8 @@ def short_name(k: str) -> str:
         return "paged_attn: merge of cut blocks"
     if "merge_rows_kernel" in k:
         return "paged_attn: merge with shared keys"
-    if "rope_kernel" in k:      # <type, pairs are halves, into a paged cache>
-        return "paged_kv_append" if re.search(r"rope_kernel(I\w+?Lb\dELb1E|<.*, true>)", k) else "rope_axes"
+    if "rope_kernel" in k:      # <type, pairs are halves, into a paged cache, heads of a thread>
+        return "paged_kv_append" if re.search(r"rope_kernel(I\w+?Lb\dELb1E|<.*, true, \d+>)", k) else "rope_axes"
     if "short_call_bf16_kernel" in k:   # whole calls of few key tiles, key ranges or whole blocks
         return "attention_short_call (bf16 MFMA)"
     if "bwd_dkv_reduce" in k:

@@ -33,6 +33,7 @@ CASES = [  # dtype, T, Hq, Hk, D, rotary, sections, layout, interleaved
     ("bf16", 9, 2, 2, 9, 2, (1,), "halves", False),                # an odd head, one pair
     ("bf16", 3000, 28, 4, 128, 128, (16, 24, 24), "pairs", False),  # several heads to a thread
     ("bf16", 2111, 28, 4, 128, 118, (16, 24, 19), "halves", False),
+    ("bf16", 8300, 28, 4, 128, 118, (16, 24, 19), "halves", False),  # more heads to a thread
     ("f32", 1, 8, 2, 128, 128, (64,), "halves", False),
     ("f32", 77, 14, 2, 64, 46, (11, 12), "pairs", False),
     ("f32", 130, 3, 1, 256, 256, (0, 100, 28), "halves", True),
@@ -129,6 +130,7 @@ def test_no_tokens_and_one_device():
     ("bf16", (28, 4), 128, 64, [500, 64, 65, 2000], [1, 1, 1, 1], True),
     ("bf16", (28, 4), 128, 16, [40, 3, 0, 17, 33], [40, 3, 0, 2, 0], True),
     ("bf16", (14, 2), 64, 32, [1200, 900], [1100, 900], True),
+    ("bf16", (28, 4), 128, 64, [7800, 900], [7600, 800], True),
     ("bf16", (4, 4), 64, 256, [300, 7], [290, 7], False),
     ("f32", (8, 2), 128, 16, [16, 1, 50], [16, 1, 35], True),
     ("f32", (2, 1), 64, 64, [130] * 300, [1] * 300, False),
