@@ -150,9 +150,15 @@ int32_t blocks16_for(int64_t rows, int32_t dtype) { return rows <= 16 ? 1 : rows
 // A call of at most this many rows a sequence is one of few rows: only such calls use shared_len.
 constexpr int64_t FEW_ROWS = 64;
 
-// A block's start and end cost about as much as this many keys, and a share of fewer keys is not worth a workgroup and a merge.
-constexpr int32_t START_KEYS = 64, MIN_SHARE = 256;
-constexpr int32_t CHUNK_START_KEYS = 128, CHUNK_MIN_SHARE = 512;
+// What starting and ending a block costs, in keys, and the least share (that cost included) worth a workgroup and a merge.  Measured over
+// 32 ... 480 keys: one token over 1,100 keys 16.4 us with 64 (and 256), 14.8 with 240 (320); eight rollouts over a shared video 36.7
+// and 33.6; fp32 chunks 74 with 64, 65 with 160, 67.5 with 240; chunks of 1 ... 301 tokens (24 sequences, heads of 64) 157 with 128
+// (512), 149 with 384 (768); a single chunk of 2,048 tokens does not mind.
+struct Costs {
+  int32_t start_keys, min_share;
+};
+constexpr Costs FEW_ROWS_COSTS[2] = {{160, 256}, {240, 320}};  // fp32, bf16
+constexpr Costs CHUNK_COSTS = {384, 768};
 
 // bf16 calls of more rows a sequence than a block of few rows holds run in blocks of PAGED_CHUNK_ROWS
 bool is_chunk(int64_t rows, int64_t num_seqs, int32_t dtype) { return dtype == PA_BF16 && rows > FEW_ROWS * num_seqs; }
@@ -194,13 +200,13 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   s.causal_cuts = chunk;
   s.inv_group = 1.0f / (float)s.group;
   s.capacity = d.max_pages_per_seq << plan.page_shift;
-  const int32_t start = chunk ? CHUNK_START_KEYS : START_KEYS, least = chunk ? CHUNK_MIN_SHARE : MIN_SHARE;
+  const Costs costs = chunk ? CHUNK_COSTS : FEW_ROWS_COSTS[d.dtype == PA_BF16];
   // No lengths of such a call can cost more than this many keys; the unit keeps that below 2^30 units.
-  const double most = ((double)rows / s.block_rows + 2.0 * (num_seqs + 1)) * s.Hkv * ((double)s.capacity + num_tokens + start + 64);
+  const double most = ((double)rows / s.block_rows + 2.0 * (num_seqs + 1)) * s.Hkv * ((double)s.capacity + num_tokens + costs.start_keys + 64);
   s.unit_shift = 4;
   while (most / (double)((int64_t)1 << s.unit_shift) > (double)(1 << 29)) ++s.unit_shift;
-  s.start_cost = (start >> s.unit_shift) + 1;
-  s.min_share = (least >> s.unit_shift) + 1;
+  s.start_cost = (costs.start_keys >> s.unit_shift) + 1;
+  s.min_share = (costs.min_share >> s.unit_shift) + 1;
   s.more_cost = (s.block_rows / s.group) >> s.unit_shift;
   s.per_group = (1.0f + 1.0f / (1 << 20)) / (float)a.groups;
   a.line = reinterpret_cast<pa::PagedLine*>(ws);
