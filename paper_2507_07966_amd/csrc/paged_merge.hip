@@ -2,9 +2,9 @@
 //
 // Without shared keys, workgroup (share, y) looks whether its share begins a block that it does not end, and merges rows of that block: the
 // last piece that share left and what the shares after it left of the same block.  With shared keys every row has
-// pieces of its own keys and of the shared ones: a workgroup per row finds both from the line.  Bound: latency; a row's D / 4 vectors are
-// spread over lanes and its pieces over groups of lanes, whose sums are joined through LDS.  Blocks of many rows have few pieces: there a
-// workgroup takes several rows at once, a lane all pieces of its vector.
+// pieces of its own keys and of the shared ones: a workgroup per row finds both from the line.  Bound: latency.  A row's D / 4 vectors are
+// spread over lanes; the groups of lanes that a workgroup has for it are split between rows and pieces, by how many pieces a row has, and
+// the sums of a row's groups are joined through LDS.
 #include <hip/hip_runtime.h>
 
 #include "paged.h"
@@ -25,22 +25,22 @@ struct Pieces {
   int32_t first_share, row;  // further pieces: slot 2 (first_share + i), row `row` of it
 };
 
-template <int D, int PARTS_>
+template <int D>
 struct Joint {
-  static constexpr int VECS = D / 4, PARTS = PARTS_;  // lanes of a row, pieces worked on at once
-  static constexpr int ROWS = THREADS / VECS / PARTS;  // rows of a workgroup
-  static_assert(PARTS == 1 || ROWS == 1, "either several pieces at once or several rows");
-  f32x4 acc[PARTS][VECS];
-  float top[PARTS], sum[PARTS];
+  static constexpr int VECS = D / 4, GROUPS = THREADS / VECS;  // lanes of a row, groups of them in a workgroup
+  f32x4 acc[GROUPS][VECS];
+  float top[GROUPS], sum[GROUPS];
 };
 
-// The row is made up of one or two lists of pieces.  With several pieces at once every thread of the workgroup calls it, for one row.
-template <typename T, int D, int PARTS>
-__device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], int lists, int64_t t, int64_t h, Joint<D, PARTS>& joint) {
-  using J = Joint<D, PARTS>;
-  const int vec = threadIdx.x % J::VECS, part = PARTS == 1 ? 0 : threadIdx.x / J::VECS;
+// This lane's vector of a row of one or two lists of pieces, `parts` groups of lanes (a power of two, in a row) to a row.  Every thread of the
+// workgroup calls it; `live`: the row exists.
+template <typename T, int D>
+__device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], int lists, int parts, bool live, int64_t t, int64_t h,
+                                 Joint<D>& joint) {
+  using J = Joint<D>;
+  const int vec = threadIdx.x % J::VECS, group = threadIdx.x / J::VECS, part = group & (parts - 1);
   const int block_rows = a.shape.block_rows;
-  const int n0 = list[0].count, n = n0 + (lists > 1 ? list[1].count : 0);
+  const int n0 = list[0].count, n = !live ? 0 : n0 + (lists > 1 ? list[1].count : 0);
   auto at = [&](int i, const float*& o, const float*& l) {
     const Pieces& p = i < n0 ? list[0] : list[1];
     const int k = i < n0 ? i : i - n0;
@@ -52,12 +52,12 @@ __device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], in
   float top = -INFINITY, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   constexpr int STEP = 4;  // pieces in flight a lane
-  for (int i0 = part; i0 < n; i0 += J::PARTS * STEP) {
+  for (int i0 = part; i0 < n; i0 += parts * STEP) {
     float l[STEP];
     f32x4 o[STEP];
 #pragma unroll
     for (int e = 0; e < STEP; ++e) {
-      const int i = i0 + e * J::PARTS;
+      const int i = i0 + e * parts;
       l[e] = -INFINITY;
       o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (i < n) {
@@ -81,67 +81,76 @@ __device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], in
       acc += w * o[e];
     }
   }
-  if constexpr (PARTS > 1) {
-    joint.acc[part][vec] = acc;
+  if (parts > 1) {
+    joint.acc[group][vec] = acc;
     if (vec == 0) {
-      joint.top[part] = top;
-      joint.sum[part] = sum;
+      joint.top[group] = top;
+      joint.sum[group] = sum;
     }
     __syncthreads();
     if (part) return;
     top = -INFINITY;
     sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) top = fmaxf(top, joint.top[p]);
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, joint.top[group + p]);
     const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-      const float w = expf(joint.top[p] - ref);
-      sum += w * joint.sum[p];
-      acc += w * joint.acc[p][vec];
+    for (int p = 0; p < parts; ++p) {
+      const float w = expf(joint.top[group + p] - ref);
+      sum += w * joint.sum[group + p];
+      acc += w * joint.acc[group + p][vec];
     }
   }
+  if (!live) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;  // 0: no piece has a key that the row sees
   write_row<T>(Place{static_cast<T*>(a.out) + (t * a.Hq + h) * D, nullptr, false}, 4 * vec, acc * inv);
   if (vec == 0 && a.lse) a.lse[h * a.shape.T + t] = (top == -INFINITY ? 0.f : top) + logf(sum);
 }
 
-// blockIdx.y: which rows of the block
-template <typename T, int D, int PARTS>
+// Groups of lanes to a row of `pieces` pieces: a lane has STEP = 4 of them in flight, and should not need a second round.
+template <int D>
+__device__ inline int parts_for(int pieces) {
+  int parts = 1;
+  while (parts < Joint<D>::GROUPS && pieces > 4 * parts) parts *= 2;
+  return parts;
+}
+
+template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void merge_cuts_kernel(const PagedArgs a) {
   const int position = blockIdx.x;
-  if (position >= a.line->active) return;
+  const int active = a.line->active;
   const PagedCut c = a.cuts[position];
-  if (c.tokens == 0) return;
-  using J = Joint<D, PARTS>;
+  if (position >= active || c.tokens == 0) return;
+  using J = Joint<D>;
   __shared__ J joint;
-  const int r = blockIdx.y * J::ROWS + (PARTS == 1 ? threadIdx.x / J::VECS : 0);
-  const int m = c.block * a.shape.block_rows + r;
-  if (m >= c.tokens * a.shape.group) return;
-  const int i = (uint32_t)m / (uint32_t)a.shape.group, j = m - i * a.shape.group;
-  const Pieces list[2] = {{c.last - c.first + 1, (2 * (int64_t)c.first + 1) * a.shape.block_rows + r, false, c.first, r}, {}};
-  merge_row<T, D, PARTS>(a, list, 1, c.token0 + i, (int64_t)c.head * a.shape.group + j, joint);
+  const int pieces = c.last - c.first + 1, parts = parts_for<D>(pieces), rows = J::GROUPS / parts;  // rows of the workgroup
+  const int left = c.tokens * a.shape.group - c.block * a.shape.block_rows;
+  const int end = left < a.shape.block_rows ? left : a.shape.block_rows;
+  for (int r0 = blockIdx.y * rows; r0 < end; r0 += gridDim.y * rows) {
+    const int r = r0 + threadIdx.x / J::VECS / parts;
+    const int m = c.block * a.shape.block_rows + r, i = (uint32_t)m / (uint32_t)a.shape.group, j = m - i * a.shape.group;
+    const Pieces list[2] = {{pieces, (2 * (int64_t)c.first + 1) * a.shape.block_rows + r, false, c.first, r}, {}};
+    merge_row<T, D>(a, list, 1, parts, r < end, c.token0 + i, (int64_t)c.head * a.shape.group + j, joint);
+    if (parts > 1) __syncthreads();
+  }
 }
 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) {
-  constexpr int PARTS = THREADS / (D / 4);
-  __shared__ Joint<D, PARTS> joint;
+  __shared__ Joint<D> joint;
   __shared__ int seq;
   const int64_t t = blockIdx.x;
   const int64_t h = blockIdx.y;
-  if (a.line->active == 0) return;
+  const PagedLine line = *a.line;
   if (threadIdx.x == 0) seq = -1;
   __syncthreads();
   for (int b = threadIdx.x; b < a.shape.B; b += THREADS)
     if (a.cu_new[b] <= t && t < a.cu_new[b + 1]) seq = b;
   __syncthreads();
   const int b = __builtin_amdgcn_readfirstlane(seq);
-  if (b < 0) return;
+  if (b < 0 || line.active == 0) return;
   PagedShape s = a.shape;
-  s.shared = a.line->shared;
-  const int32_t share = a.line->share;
+  s.shared = line.shared;
+  const int32_t share = line.share;
   const int head = (int)h / s.group, j = (int)h - head * s.group;
   auto pieces = [&](const Segment& g, int32_t start, bool shared) {
     const uint32_t m = (uint32_t)(t - g.token0) * s.group + j;
@@ -153,7 +162,7 @@ __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) 
   };
   const Segment own = load_segment(a, s, b + 1), all = load_segment(a, s, 0);
   const Pieces list[2] = {pieces(own, a.seg_start[b + 1], false), t < all.tokens ? pieces(all, a.seg_start[0], true) : Pieces{}};
-  merge_row<T, D, PARTS>(a, list, 2, t, h, joint);
+  merge_row<T, D>(a, list, 2, Joint<D>::GROUPS, true, t, h, joint);
 }
 
 template <typename T, int D>
@@ -161,11 +170,10 @@ int launch(const PagedArgs& a, hipStream_t s) {
   if (a.shared_len) {
     merge_rows_kernel<T, D><<<dim3((unsigned)a.shape.T, (unsigned)a.Hq), THREADS, 0, s>>>(a);
   } else {
+    // A block's rows are dealt to up to 16 workgroups: all rows of short blocks at once where they have many pieces
     const int64_t rows = (int64_t)a.shape.T * a.shape.group;  // of a kv head, in all
     const int most = rows < a.shape.block_rows ? (int)rows : a.shape.block_rows;
-    constexpr int LANES = THREADS / (D / 4);
-    if (a.shape.block_rows > 64) merge_cuts_kernel<T, D, 1><<<dim3((unsigned)a.groups, (unsigned)((most + LANES - 1) / LANES)), THREADS, 0, s>>>(a);
-    else merge_cuts_kernel<T, D, LANES><<<dim3((unsigned)a.groups, (unsigned)most), THREADS, 0, s>>>(a);
+    merge_cuts_kernel<T, D><<<dim3((unsigned)a.groups, (unsigned)(most < 16 ? most : 16)), THREADS, 0, s>>>(a);
   }
   return (int)hipGetLastError();
 }
