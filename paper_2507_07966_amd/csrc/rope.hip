@@ -6,8 +6,8 @@
 // Mapping: a head's channels are split into units of W channel pairs (16 bytes of each of the two channels of a pair, or of W / 2
 // neighbouring pairs), of W channels that pass through, and of single pairs and channels where a size is no multiple of W.
 // A thread owns one unit of one token, forms the unit's sines and cosines once in registers, and turns that unit of HPT heads: four or
-// eight in large calls, one in small ones, where latency counts.  The heads' loads are issued before the sines are worked out
-// (32,768 tokens, 28 + 4 heads of 128, bf16: 132 -> 111 us, 4.8 TB/s).  Large calls store past the caches (139 -> 132 us before that;
+// eight in large calls, two in small ones, where latency counts.  The heads' loads are issued before the sines are worked out
+// (32,768 tokens, 28 + 4 heads of 128, bf16: 132 -> 111 us, 4.8 TB/s).  The largest calls store past the caches (139 -> 132 us before that;
 // appended chunks, whose values are only copied, 50 -> 37 us).  Vector accesses are declared with the alignment of an element, so slices at any offset take the same path.
 #include <hip/hip_runtime.h>
 
@@ -64,6 +64,7 @@ struct Units {
 
 struct RopeKernelArgs {
   RopeArgs a;
+  uint32_t axis_bits[PA_ROPE_MAX_PAIRS / 16];  // pair_axis, two bits a pair: in scalar registers, unlike an array indexed by lane
   int tokens;  // per workgroup
   int groups;  // of heads that a token is split over: thread (token, group g, unit) does heads g, g + groups, ...
 };
@@ -76,7 +77,7 @@ __device__ inline void store(VU* p, V x) {
 template <typename T, bool HALVES, bool APPEND, int HPT>
 __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) {
   constexpr int W = 16 / sizeof(T);
-  constexpr bool LARGE = HPT > 1;
+  constexpr bool PAST = HPT > 4;  // stores past the caches: results that these cannot hold anyway (44 MB of fp32, kept in them: 13.9 -> 12.3 us)
   using V = typename Vec<T, W>::type;
   using VU = typename Vec<T, W>::unaligned;
   const RopeArgs& a = ka.a;
@@ -88,9 +89,10 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) 
   const int ntok = (int)(a.T - t0 < ka.tokens ? a.T - t0 : ka.tokens);
   if (ntok <= 0) return;
 
-  // append: the cache row (page, slot) of each of the workgroup's tokens, -1: not stored, -2: padding behind the last sequence
+  // append: the cache row (page, slot) of each of the workgroup's tokens, -1: not stored, -2: padding behind the last sequence; worked out
+  // while the first round's loads are under way
   __shared__ int64_t place[APPEND ? THREADS : 1];
-  if (APPEND) {
+  auto find_places = [&]() {
     if ((int)threadIdx.x < ntok) place[threadIdx.x] = -2;
     __syncthreads();
     for (int b = threadIdx.x; b < a.B; b += THREADS) {
@@ -110,15 +112,16 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) 
       }
     }
     __syncthreads();
-  }
+  };
 
-  for (int idx = threadIdx.x; idx < ntok * per_token; idx += THREADS) {
+  const int work = ntok * per_token;
+  for (int base = 0; base < work; base += THREADS) {
+    const bool live = base + (int)threadIdx.x < work;
+    const int idx = live ? base + threadIdx.x : 0;
     const int tok = idx / per_token, rest = idx - tok * per_token;
     const int g = rest / U;
     int u = rest - g * U;
     const int64_t t = t0 + tok;
-    const int64_t at = APPEND ? place[tok] : 0;
-    if (APPEND && at == -2) continue;
     UnitKind kind;
     int ca, cb;  // first channel of the unit and of its partners
     if (u < units.turn) {
@@ -138,30 +141,15 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) 
       ca = cb = R + units.pass * W + (u - units.pass);
     }
     const T* src[HPT];
-    T* dst[HPT];
-    bool turn[HPT];
     V xa[HPT], xb[HPT];
 #pragma unroll
     for (int i = 0; i < HPT; ++i) {
       const int h = g + i * ka.groups;
       src[i] = nullptr;
-      turn[i] = true;
-      if (h < a.Hq) {
-        src[i] = static_cast<const T*>(a.q) + t * a.q_stride + h * D;
-        dst[i] = static_cast<T*>(a.q_out) + t * a.q_out_stride + h * D;
-      } else if (h < a.Hq + a.Hk) {
-        const int hk = h - a.Hq;
-        src[i] = static_cast<const T*>(a.k) + t * a.k_stride + hk * D;
-        dst[i] = APPEND ? static_cast<T*>(a.k_cache) + (at + ((int64_t)hk << a.page_shift)) * D
-                        : static_cast<T*>(a.k_out) + t * a.k_out_stride + hk * D;
-        if (APPEND && at < 0) src[i] = nullptr;
-      } else if (APPEND && h < heads) {
-        const int hv = h - a.Hq - a.Hk;
-        src[i] = static_cast<const T*>(a.v) + t * a.v_stride + hv * D;
-        dst[i] = static_cast<T*>(a.v_cache) + (at + ((int64_t)hv << a.page_shift)) * D;
-        turn[i] = false;
-        if (at < 0) src[i] = nullptr;
-      }
+      if (!live) continue;
+      if (h < a.Hq) src[i] = static_cast<const T*>(a.q) + t * a.q_stride + h * D;
+      else if (h < a.Hq + a.Hk) src[i] = static_cast<const T*>(a.k) + t * a.k_stride + (h - a.Hq) * D;
+      else if (APPEND && h < heads) src[i] = static_cast<const T*>(a.v) + t * a.v_stride + (h - a.Hq - a.Hk) * D;
       if (!src[i]) continue;
       if (kind == TURN || kind == PASS) {
         xa[i] = *reinterpret_cast<const VU*>(src[i] + ca);
@@ -173,27 +161,43 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) 
     }
     constexpr int N = HALVES ? W : W / 2;  // pairs of a full unit
     float cs[N], sn[N];
-    if (kind == TURN || kind == TURN_ONE) {
+    if (live && (kind == TURN || kind == TURN_ONE)) {
       const int n = kind == TURN ? N : 1;
-      const int pair0 = HALVES ? ca : ca / 2;
+      const int pair0 = HALVES ? ca : ca / 2;  // a full unit's pairs are within one word
+      uint32_t bits = ka.axis_bits[0];
+      for (int w = 1; w * 32 < R; ++w) bits = pair0 >> 4 == w ? ka.axis_bits[w] : bits;
+      bits >>= 2 * (pair0 & 15);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         cs[e] = 1.f;
         sn[e] = 0.f;
         if (e < n) {
-          angle_cos_sin(a.positions[(int64_t)a.rope.pair_axis[pair0 + e] * a.T + t], a.inv_freq[pair0 + e], cs[e], sn[e]);
+          angle_cos_sin(a.positions[(int64_t)(bits >> 2 * e & 3) * a.T + t], a.inv_freq[pair0 + e], cs[e], sn[e]);
           sn[e] *= a.sign;
         }
       }
     }
+    if (APPEND && base == 0) find_places();
+    const int64_t at = APPEND ? place[tok] : 0;
 #pragma unroll
     for (int i = 0; i < HPT; ++i) {
-      if (!src[i]) continue;
-      T* y = dst[i];
-      if (kind == PASS || (kind == TURN && !turn[i])) {
-        store<LARGE>(reinterpret_cast<VU*>(y + ca), xa[i]);
-        if (HALVES && kind == TURN) store<LARGE>(reinterpret_cast<VU*>(y + cb), xb[i]);
-      } else if (kind == PASS_ONE || !turn[i]) {
+      const int h = g + i * ka.groups;
+      if (!src[i] || (APPEND && at == -2)) continue;
+      T* y;
+      const bool turn = h < a.Hq + a.Hk;
+      if (h < a.Hq) {
+        y = static_cast<T*>(a.q_out) + t * a.q_out_stride + h * D;
+      } else if (!APPEND) {
+        y = static_cast<T*>(a.k_out) + t * a.k_out_stride + (h - a.Hq) * D;
+      } else {
+        if (at < 0) continue;
+        const int hk = turn ? h - a.Hq : h - a.Hq - a.Hk;
+        y = static_cast<T*>(turn ? a.k_cache : a.v_cache) + (at + ((int64_t)hk << a.page_shift)) * D;
+      }
+      if (kind == PASS || (kind == TURN && !turn)) {
+        store<PAST>(reinterpret_cast<VU*>(y + ca), xa[i]);
+        if (HALVES && kind == TURN) store<PAST>(reinterpret_cast<VU*>(y + cb), xb[i]);
+      } else if (kind == PASS_ONE || !turn) {
         y[ca] = xa[i][0];
         if (kind == TURN_ONE) y[cb] = xb[i][0];
       } else if (kind == TURN) {
@@ -211,8 +215,8 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(const RopeKernelArgs ka) 
             ya[(2 * e + 1) % W] = (T)y1;
           }
         }
-        store<LARGE>(reinterpret_cast<VU*>(y + ca), ya);
-        if (HALVES) store<LARGE>(reinterpret_cast<VU*>(y + cb), yb);
+        store<PAST>(reinterpret_cast<VU*>(y + ca), ya);
+        if (HALVES) store<PAST>(reinterpret_cast<VU*>(y + cb), yb);
       } else {
         const float x0 = (float)xa[i][0], x1 = (float)xb[i][0];
         y[ca] = (T)(x0 * cs[0] - x1 * sn[0]);
@@ -226,12 +230,13 @@ template <typename T, bool HALVES, bool APPEND>
 int launch(const RopeArgs& a, void* stream) {
   const Units<16 / (int)sizeof(T), HALVES> units(a.rope.head_dim, a.rope.rotary_dim);
   const int heads = a.Hq + a.Hk + a.Hv;
-  RopeKernelArgs k;
+  RopeKernelArgs k{};
   k.a = a;
+  for (int i = 0; i < a.rope.rotary_dim / 2; ++i) k.axis_bits[i / 16] |= (uint32_t)a.rope.pair_axis[i] << (2 * (i % 16));
   // As many heads as leave a few wavefronts to every SIMD: 8 from 2^21 units on (2^18 threads), 4 from 2^18 on.  In fp32, 5,377 tokens, 14 +
   // 2 heads of 64 (2^20.6 units): 12.7 us with 4, 14.0 with 8; bf16, 18,432 tokens, 28 + 4 of 128 (2^22.2): 68.6 and 61.3.
   const int64_t work = a.T * heads * units.count();
-  const int hpt = work >= (1 << 21) ? 8 : work >= (1 << 18) ? 4 : 1;
+  const int hpt = work >= (1 << 21) ? 8 : work >= (1 << 18) ? 4 : 2;
   k.groups = (heads + hpt - 1) / hpt;
   const int per_token = units.count() * k.groups;
   k.tokens = per_token >= THREADS ? 1 : THREADS / per_token;
@@ -241,7 +246,7 @@ int launch(const RopeArgs& a, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (hpt == 8) rope_kernel<T, HALVES, APPEND, 8><<<dim3(gx, gy), THREADS, 0, st>>>(k);
   else if (hpt == 4) rope_kernel<T, HALVES, APPEND, 4><<<dim3(gx, gy), THREADS, 0, st>>>(k);
-  else rope_kernel<T, HALVES, APPEND, 1><<<dim3(gx, gy), THREADS, 0, st>>>(k);
+  else rope_kernel<T, HALVES, APPEND, 2><<<dim3(gx, gy), THREADS, 0, st>>>(k);
   return (int)hipGetLastError();
 }
 
