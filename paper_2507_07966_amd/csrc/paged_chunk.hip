@@ -94,7 +94,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
     const int first_limit = __builtin_amdgcn_readfirstlane(limit[0]);
 
     // Where a wavefront's rows of tile t are: found for K, and used for V one step later.  The page number is read two steps before.
-    const uint32_t page_bytes = (uint32_t)((shape.Hkv << a.page_shift) * ROWB);
+    const uint32_t page_bytes = ((uint32_t)shape.Hkv << a.page_shift) * (uint32_t)ROWB;
     const int64_t head_bytes = ((int64_t)walk.head << a.page_shift) * ROWB;
     const int wave_key = first_key + wave * WAVE_KEYS;
     int last_key = first_key + tiles * TILE < p.key_end ? first_key + tiles * TILE : p.key_end;

@@ -218,7 +218,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
     const int stages = span > 0 ? (span + WAVES * KEYS - 1) / (WAVES * KEYS) : 0;
     const int key_base = first_key + wave * KEYS;
 
-    const uint32_t page_bytes = (uint32_t)((shape.Hkv << a.page_shift) * ROWB);
+    const uint32_t page_bytes = ((uint32_t)shape.Hkv << a.page_shift) * (uint32_t)ROWB;
     const int64_t head_bytes = ((int64_t)walk.head << a.page_shift) * ROWB;
     int first_lost = last_key > shape.capacity ? shape.capacity : 0x7fffffff;  // smallest key without a page: rows that see it become NaN
     const int end = last_key < shape.capacity ? last_key : shape.capacity;

@@ -20,6 +20,8 @@ CASES = {
     "chunk_from_nothing": ("bf16", (4, 4), 64, 16, [401], [401], 0),
     "chunk_d64": ("bf16", (14, 2), 64, 64, [1500, 90], [130, 90], 0),
     "mixed": ("bf16", (28, 4), 128, 64, [600, 311, 64, 900, 100], [200, 1, 1, 77, 100], 0),
+    "many_chunks": ("bf16", (4, 1), 64, 16, [20 + i % 21 for i in range(600)], [17] * 600, 0),
+    "tokens_of_two_blocks": ("bf16", (32, 2), 128, 64, [700, 65], [2, 1], 0),
     "many_sequences": ("bf16", (2, 2), 64, 16, list(range(1, 301)), [1] * 300, 0),
     "shared": ("bf16", (28, 4), 128, 64, [1050, 1100, 1025, 1400], [1] * 4, 1024),
     "shared_few": ("bf16", (14, 2), 64, 16, [700, 660, 671], [4, 1, 3], 640),
@@ -58,12 +60,12 @@ def test_nothing_behind_the_last_key_reaches_a_result(dtype, dim, new):
     x.check(*x.attend(), want)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("new", [[1, 1, 1, 1, 1], [70, 1, 33, 40, 2]])
-def test_rows_without_keys_and_keys_without_pages(dtype, new):
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1, 1], [70, 1, 33, 40, 2], [70, 31, 33, 40, 60]])
+def test_rows_without_keys_and_keys_without_pages(dtype, dim, new):
     """A sequence shorter than its new tokens: zeros and -inf; a missing page, a length beyond the table: NaN for the rows that see it only."""
     lens = [50 if new[0] > 1 else 0, 300, 40, 45, 70]
-    x = Paged(dtype, (4, 2), 64, 16, lens, new, pad=2, seed=7, wide=0)
+    x = Paged(dtype, (16, 2) if dtype == "bf16" else (4, 2), dim, 16, lens, new, pad=2, seed=7, wide=0)
     x.lens[0] = 45 if new[0] > 1 else 0       # 70 new tokens, 45 in all: 25 rows see nothing
     x.table[1, 3] = -5
     x.table[2, 1] = x.pages
@@ -80,10 +82,10 @@ def test_rows_without_keys_and_keys_without_pages(dtype, new):
     assert np.isneginf(lse[:, 0]).all()
 
 
-@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 120), ("f32", 5)])
-def test_large_and_late_scores(dtype, new):
-    """Scores of hundreds, the largest last: the running maximum moves at every tile."""
-    x = Paged(dtype, (4, 2), 64, 64, [800, 330], [new, new], seed=8)
+@pytest.mark.parametrize("dtype,dim,new", [("bf16", 64, 1), ("bf16", 64, 120), ("f32", 64, 5), ("bf16", 128, 12), ("bf16", 128, 30), ("bf16", 128, 150)])
+def test_large_and_late_scores(dtype, dim, new):
+    """Scores of hundreds, the largest last: the running maximum moves at every tile, and chunks are done again with their true maxima."""
+    x = Paged(dtype, (4, 2), dim, 64, [800, 330], [new, new], seed=8)
     grow = np.zeros((x.pages, 1, x.page, 1))
     for b, n in enumerate(x.lens):
         for j in range(n):
@@ -175,4 +177,61 @@ def test_two_streams_with_workspaces_of_their_own():
             pa.paged_attn_forward(plan, qs[i], *dev, got[i], None, wss[i], stream=s)
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    plan.destroy()
+
+
+def test_results_are_reproducible():
+    x = Paged("bf16", (28, 4), 128, 64, [9000, 333, 4000], [1, 1, 1], seed=14)
+    y = Paged("bf16", (28, 4), 128, 64, [2000, 900], [260, 200], seed=15)
+    for z in (x, y):
+        a, b = z.attend(), z.attend()
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+def test_lengths_that_fall_and_empty_calls_compute_nothing():
+    import torch
+    import paper_2507_07966_amd as pa
+    for shared in (None, 16):
+        x = Paged("bf16", (4, 2), 64, 16, [100, 50, 70], [2, 3, 1], seed=16)
+        x.cu = np.array([0, 4, 2, 6], dtype=np.int32)
+        out, lse = x.attend(shared_len=shared)
+        assert (out == 7).all() and (lse == 7).all()
+    plan = x.plan()
+    dev = x.upload()
+    out = torch.full((0, 4, 64), 7.0, device="cuda", dtype=torch.bfloat16)
+    pa.paged_attn_forward(plan, out, *dev, out, None, torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda"))
+    q = torch.full((3, 4, 64), 7.0, device="cuda", dtype=torch.bfloat16)
+    none = dev[0], dev[1], dev[2][:0], dev[3][:0], dev[4][:1]
+    pa.paged_attn_forward(plan, q, *none, q, None, torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    assert (q == 7).all()
+    plan.destroy()
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [1, 1]), ("bf16", [90, 40]), ("f32", [1, 2])])
+def test_caches_beyond_four_gibibytes(dtype, new):
+    """Pages at the end of caches of more than 2^32 bytes each, appended to and read."""
+    import torch
+    import paper_2507_07966_amd as pa
+    x = Paged(dtype, (8, 2), 128, 64, [200, 130], new, seed=17)
+    size = 2 if dtype == "bf16" else 4
+    many = (1 << 32) // (2 * 64 * 128 * size) + x.pages + 5
+    shift = many - x.pages
+    plan = x.plan(num_pages=many)
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    kc, vc = (torch.empty(many, 2, 64, 128, dtype=tdt, device="cuda") for _ in range(2))
+    kc[shift:], vc[shift:] = gpu(x.k, dtype), gpu(x.v, dtype)
+    rows = [(t, b, int(x.lens[b] - x.cu[b + 1] + t)) for b in range(2) for t in range(x.cu[b], x.cu[b + 1])]
+    k = np.stack([x.k[x.table[b, p // 64], :, p % 64] for _, b, p in rows])
+    v = np.stack([x.v[x.table[b, p // 64], :, p % 64] for _, b, p in rows])
+    for _, b, p in rows:   # wiped, and appended again
+        kc[shift + int(x.table[b, p // 64]), :, p % 64] = 9
+        vc[shift + int(x.table[b, p // 64]), :, p % 64] = 9
+    table = gpu(np.where(x.table >= 0, x.table + shift, -1).astype(np.int32))
+    args = kc, vc, table, gpu(x.lens), gpu(x.cu)
+    pa.paged_kv_append(plan, gpu(k, dtype), gpu(v, dtype), *args)
+    out, lse = torch.empty(x.tokens, 8, 128, dtype=tdt, device="cuda"), torch.empty(8, x.tokens, device="cuda")
+    pa.paged_attn_forward(plan, gpu(x.q, dtype), *args, out, lse, torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda"))
+    assert np.array_equal(host(kc[shift:]), x.k) and np.array_equal(host(vc[shift:]), x.v)
+    x.check(host(out), host(lse))
     plan.destroy()

@@ -73,7 +73,7 @@ def test_rope_is_the_definition(case, backward):
         assert np.array_equal(host(y)[:, :, rope.rotary_dim:], x[:, :, rope.rotary_dim:])
 
 
-@pytest.mark.parametrize("case", [CASES[1], CASES[2], CASES[9]], ids=lambda c: f"{c[0]}-{c[1]}")
+@pytest.mark.parametrize("case", [CASES[1], CASES[2], CASES[10]], ids=lambda c: f"{c[0]}-{c[1]}")
 def test_rope_of_slices_in_place_and_of_far_positions(case):
     """Slices of a fused projection that start at any element, results over the inputs, positions up to 2^31, and nothing beside the
     slices written."""
