@@ -75,11 +75,19 @@ __device__ inline int32_t shared_keys(const PagedArgs& a) {
   if (!a.shared_len) return 0;
   return whole_pages(a.shape, read_const(a.shared_len, 0), a.page_shift);
 }
-__device__ inline Segment load_segment(const PagedArgs& a, const PagedShape& s, int i) {
+// What segment i is made from: read before `shared` is known, so that the reads do not wait for each other.
+struct Lengths {
+  int32_t cu0, cu1, len;
+};
+__device__ inline Lengths read_lengths(const PagedArgs& a, int i) {
   const int with = a.shared_len ? 1 : 0;
-  if (i < with) return shared_segment(s, read_const(a.cu_new, s.B));
-  return own_segment(s, read_const(a.cu_new, i - with), read_const(a.cu_new, i - with + 1), read_const(a.seq_lens, i - with));
+  if (i < with) return Lengths{0, read_const(a.cu_new, a.shape.B), 0};
+  return Lengths{read_const(a.cu_new, i - with), read_const(a.cu_new, i - with + 1), read_const(a.seq_lens, i - with)};
 }
+__device__ inline Segment segment_of(const PagedArgs& a, const PagedShape& s, int i, const Lengths& l) {
+  return a.shared_len && i == 0 ? shared_segment(s, l.cu1) : own_segment(s, l.cu0, l.cu1, l.len);
+}
+__device__ inline Segment load_segment(const PagedArgs& a, const PagedShape& s, int i) { return segment_of(a, s, i, read_lengths(a, i)); }
 
 // The last key that a new token sees, at most the one behind the table; -1: none.
 __device__ inline int32_t row_limit(const PagedShape& s, const Segment& g, int32_t token) {
@@ -193,6 +201,8 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   __shared__ Segment found;
   __shared__ int32_t found_segment, first_seq, falls;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Lengths mine{0, 0, 0};
+  if (tid < a.shape.B + (a.shared_len ? 1 : 0)) mine = read_lengths(a, tid);
   w.shape = a.shape;
   w.shape.shared = shared_keys(a);
   const int with = a.shared_len ? 1 : 0;
@@ -210,7 +220,7 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
     const int i = base + tid;
     cost = 0;
     if (i < w.segments) {
-      g = load_segment(a, w.shape, i);
+      g = segment_of(a, w.shape, i, base == 0 ? mine : read_lengths(a, i));
       if (g.cost < 0) falls = 1;
       cost = g.cost < 0 ? 0 : w.shape.Hkv * g.cost;
       if (i >= with && cost > 0) atomicMin(&first_seq, i - with);

@@ -32,9 +32,9 @@ struct Joint {
   float top[GROUPS], sum[GROUPS];
 };
 
-// This lane's vector of a row of one or two lists of pieces, `parts` groups of lanes (a power of two, in a row) to a row.  Every thread of the
+// This lane's vector of a row of one or two lists of pieces, STEP of which it has in flight, `parts` groups of lanes (a power of two, in a row) to a row.  Every thread of the
 // workgroup calls it; `live`: the row exists.
-template <typename T, int D>
+template <typename T, int D, int STEP>
 __device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], int lists, int parts, bool live, int64_t t, int64_t h,
                                  Joint<D>& joint) {
   using J = Joint<D>;
@@ -51,7 +51,6 @@ __device__ inline void merge_row(const PagedArgs& a, const Pieces (&list)[2], in
   };
   float top = -INFINITY, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int STEP = 4;  // pieces in flight a lane
   for (int i0 = part; i0 < n; i0 += parts * STEP) {
     float l[STEP];
     f32x4 o[STEP];
@@ -129,7 +128,7 @@ __global__ __launch_bounds__(THREADS) void merge_cuts_kernel(const PagedArgs a) 
     const int r = r0 + threadIdx.x / J::VECS / parts;
     const int m = c.block * a.shape.block_rows + r, i = (uint32_t)m / (uint32_t)a.shape.group, j = m - i * a.shape.group;
     const Pieces list[2] = {{pieces, (2 * (int64_t)c.first + 1) * a.shape.block_rows + r, false, c.first, r}, {}};
-    merge_row<T, D>(a, list, 1, parts, r < end, c.token0 + i, (int64_t)c.head * a.shape.group + j, joint);
+    merge_row<T, D, 4>(a, list, 1, parts, r < end, c.token0 + i, (int64_t)c.head * a.shape.group + j, joint);
     if (parts > 1) __syncthreads();
   }
 }
@@ -137,14 +136,24 @@ __global__ __launch_bounds__(THREADS) void merge_cuts_kernel(const PagedArgs a) 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) {
   __shared__ Joint<D> joint;
-  __shared__ int seq;
+  __shared__ int seq, own_start;
+  __shared__ Lengths own_lengths;
   const int64_t t = blockIdx.x;
   const int64_t h = blockIdx.y;
   const PagedLine line = *a.line;
+  const int32_t all_start = a.seg_start[0];
+  const Lengths all_lengths = read_lengths(a, 0);
   if (threadIdx.x == 0) seq = -1;
   __syncthreads();
-  for (int b = threadIdx.x; b < a.shape.B; b += THREADS)
-    if (a.cu_new[b] <= t && t < a.cu_new[b + 1]) seq = b;
+  for (int b = threadIdx.x; b < a.shape.B; b += THREADS) {
+    const Lengths l = read_lengths(a, b + 1);
+    const int32_t start = a.seg_start[b + 1];
+    if (l.cu0 <= t && t < l.cu1) {
+      seq = b;
+      own_lengths = l;
+      own_start = start;
+    }
+  }
   __syncthreads();
   const int b = __builtin_amdgcn_readfirstlane(seq);
   if (b < 0 || line.active == 0) return;
@@ -160,9 +169,9 @@ __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) 
     if (first == last) return Pieces{1, ((shared ? (int64_t)s.T : 0) + t) * a.Hq + h, true, first, r};
     return Pieces{last - first + 1, (2 * (int64_t)first + 1) * s.block_rows + r, false, first, r};
   };
-  const Segment own = load_segment(a, s, b + 1), all = load_segment(a, s, 0);
-  const Pieces list[2] = {pieces(own, a.seg_start[b + 1], false), t < all.tokens ? pieces(all, a.seg_start[0], true) : Pieces{}};
-  merge_row<T, D>(a, list, 2, Joint<D>::GROUPS, true, t, h, joint);
+  const Segment own = segment_of(a, s, b + 1, own_lengths), all = segment_of(a, s, 0, all_lengths);
+  const Pieces list[2] = {pieces(own, own_start, false), t < all.tokens ? pieces(all, all_start, true) : Pieces{}};
+  merge_row<T, D, 8>(a, list, 2, Joint<D>::GROUPS, true, t, h, joint);
 }
 
 template <typename T, int D>
