@@ -62,7 +62,13 @@ struct PagedArgs {
   float* rows_lse;         // [2][T * Hq]
 };
 int launch_paged_rows(const PagedArgs& a, void* stream);   // calls of few rows a sequence, and fp32
-int paged_rows_tile_shift(int32_t dtype, int32_t D);       // log2 of the keys that its wavefronts share out in a step
+// Its wavefronts, and the bytes of keys (and of values) that one of them has in a step: together the keys of a tile
+constexpr int PAGED_ROWS_WAVES = 4, PAGED_ROWS_HALF_STAGE = 8192;
+inline int paged_rows_tile_shift(int32_t dtype, int32_t D) {
+  int shift = 0;
+  while ((D * (dtype == PA_BF16 ? 2 : 4)) << shift < PAGED_ROWS_WAVES * PAGED_ROWS_HALF_STAGE) ++shift;
+  return shift;
+}
 constexpr int PAGED_CHUNK_ROWS = 256, PAGED_CHUNK_TILE_SHIFT = 6;
 int launch_paged_chunk(const PagedArgs& a, void* stream);  // bf16 calls of many rows a sequence
 int launch_paged_merge(const PagedArgs& a, void* stream);

@@ -209,6 +209,7 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   s.min_share = (costs.min_share >> s.unit_shift) + 1;
   s.more_cost = (s.block_rows / s.group) >> s.unit_shift;
   s.per_group = (1.0f + 1.0f / (1 << 20)) / (float)a.groups;
+  if (!ws) return a;  // the schedule alone
   a.line = reinterpret_cast<pa::PagedLine*>(ws);
   a.seg_start = reinterpret_cast<int32_t*>(ws + plan.off_seg_start);
   a.cuts = reinterpret_cast<pa::PagedCut*>(ws + plan.off_cuts);

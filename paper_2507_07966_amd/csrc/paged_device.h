@@ -197,7 +197,7 @@ struct Walk {
 template <int THREADS>
 __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   constexpr int WAVES = THREADS / 64;
-  __shared__ int32_t wave_cost[WAVES], found_start;
+  __shared__ uint32_t wave_cost[WAVES], found_start;  // (unsigned: where cu_new falls the sums mean nothing)
   __shared__ Segment found;
   __shared__ int32_t found_segment, first_seq, falls;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -213,7 +213,7 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   }
   __syncthreads();
   // Two rounds over the segments where they are more than the threads: the sum of all costs, then the share's segment.
-  int32_t total = 0, start = 0, cost = 0;
+  uint32_t total = 0, start = 0, cost = 0;
   Segment g;
   const int lanes = w.segments < 64 ? w.segments : 64;
   auto round = [&](int base) {  // start and cost of segment base + tid; total: those before base, and then with this round's
@@ -222,17 +222,17 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
     if (i < w.segments) {
       g = segment_of(a, w.shape, i, base == 0 ? mine : read_lengths(a, i));
       if (g.cost < 0) falls = 1;
-      cost = g.cost < 0 ? 0 : w.shape.Hkv * g.cost;
+      cost = g.cost < 0 ? 0u : (uint32_t)(w.shape.Hkv * g.cost);
       if (i >= with && cost > 0) atomicMin(&first_seq, i - with);
     }
-    int32_t sum = cost;
+    uint32_t sum = cost;
     for (int d = 1; d < lanes; d *= 2) {
-      const int32_t up = __shfl_up(sum, d);
+      const uint32_t up = __shfl_up(sum, d);
       if (lane >= d) sum += up;
     }
     if (lane == lanes - 1) wave_cost[wave] = sum;
     __syncthreads();
-    int32_t before = 0, all = 0;
+    uint32_t before = 0, all = 0;
 #pragma unroll
     for (int v = 0; v < WAVES; ++v) {
       before += v < wave ? wave_cost[v] : 0;
@@ -244,20 +244,20 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   };
   for (int base = 0; base < w.segments; base += THREADS) {
     round(base);
-    if (blockIdx.x == 0 && with && base + tid < w.segments) a.seg_start[base + tid] = start;
+    if (blockIdx.x == 0 && with && base + tid < w.segments) a.seg_start[base + tid] = (int32_t)start;
   }
-  total = __builtin_amdgcn_readfirstlane(falls ? 0 : total);
-  w.share = share_of(w.shape, total);
-  const int32_t active = active_of(total, w.share);
+  const int32_t length = __builtin_amdgcn_readfirstlane(falls ? 0 : (int32_t)total);
+  w.share = share_of(w.shape, length);
+  const int32_t active = active_of(length, w.share);
   if (blockIdx.x == 0 && tid == 0) *a.line = PagedLine{w.share, active, w.shape.shared};
   w.position = position_of(blockIdx.x, active, a.xcd_shift);
   if (w.position < 0) return false;
   w.x = w.position * w.share;
-  w.x_end = w.x + w.share < total ? w.x + w.share : total;
+  w.x_end = w.x + w.share < length ? w.x + w.share : length;
   if (w.segments > THREADS) total = 0;
   for (int base = 0; base < w.segments; base += THREADS) {
     if (w.segments > THREADS) round(base);
-    if (start <= w.x && w.x < start + cost) {
+    if (start <= (uint32_t)w.x && (uint32_t)w.x < start + cost) {
       found_segment = base + tid;
       found_start = start;
       found = g;
@@ -274,7 +274,7 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   w.seg.first_cost = __builtin_amdgcn_readfirstlane(found.first_cost);
   w.seg.more_cost = __builtin_amdgcn_readfirstlane(found.more_cost);
   w.seg.cost = __builtin_amdgcn_readfirstlane(found.cost);
-  const int32_t seg_start = __builtin_amdgcn_readfirstlane(found_start);
+  const int32_t seg_start = __builtin_amdgcn_readfirstlane((int32_t)found_start);
   w.head = __builtin_amdgcn_readfirstlane(div_small(w.x - seg_start, w.seg.cost));
   w.head_start = seg_start + w.head * w.seg.cost;
   w.block_index = __builtin_amdgcn_readfirstlane(block_at(w.seg, w.x - w.head_start));

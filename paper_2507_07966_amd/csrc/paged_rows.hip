@@ -31,8 +31,8 @@ namespace {
 
 using namespace mt;
 
-constexpr int WAVES = 4, THREADS = WAVES * 64, STAGES = 2;
-constexpr int HALF_STAGE = 8192;  // bytes of keys, and of values
+constexpr int WAVES = PAGED_ROWS_WAVES, THREADS = WAVES * 64, STAGES = 2;
+constexpr int HALF_STAGE = PAGED_ROWS_HALF_STAGE;  // bytes of keys, and of values
 constexpr int LOADS = 2 * HALF_STAGE / 1024;  // of a stage
 
 // What differs between the data types: the operands of the two products.
@@ -409,12 +409,6 @@ int launch_paged_rows(const PagedArgs& a, void* stream) {
 #undef PA_ROWS_D
 #undef PA_ROWS
   return (int)hipGetLastError();
-}
-
-int paged_rows_tile_shift(int32_t dtype, int32_t D) {
-  int shift = 0;
-  while ((D * (dtype == PA_BF16 ? 2 : 4)) << shift < WAVES * HALF_STAGE) ++shift;
-  return shift;
 }
 
 }  // namespace pa

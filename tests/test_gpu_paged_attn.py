@@ -26,6 +26,8 @@ CASES = {
     "shared": ("bf16", (28, 4), 128, 64, [1050, 1100, 1025, 1400], [1] * 4, 1024),
     "shared_few": ("bf16", (14, 2), 64, 16, [700, 660, 671], [4, 1, 3], 640),
     "shared_chunk": ("bf16", (8, 2), 128, 32, [700, 460], [200, 40], 320),
+    "wide_group_chunk": ("bf16", (300, 1), 64, 16, [90, 40], [2, 1], 0),   # a token's rows fill more than a block
+    "f32_wide_group": ("f32", (40, 1), 64, 16, [90, 40], [2, 1], 0),
     "f32_token": ("f32", (8, 2), 128, 16, [1, 600, 130], [1] * 3, 0),
     "f32_chunk": ("f32", (8, 2), 128, 32, [330, 100], [130, 100], 0),
     "f32_d64": ("f32", (14, 2), 64, 64, [500, 65], [9, 1], 0),
