@@ -44,14 +44,14 @@ struct CoreBf16 {
   f32x4 O[CB][NQ];
   int koff[KS], vtr[CB];
   __device__ static int swizzle(int row) { return swizzle16(row, ROWB); }
+  // (the swizzle is an exclusive or on the chunk's bits, so the addresses of a lane differ by one, too)
   __device__ void init(int l16, int g4) {
+    const int k0 = l16 * ROWB + ((g4 ^ swizzle(l16)) << 4), r = 4 * g4 + (l16 >> 2);
+    const int v0 = r * ROWB + ((((l16 & 3) >> 1) ^ swizzle(r)) << 4) + (l16 & 1) * 8;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) koff[ks] = l16 * ROWB + (((4 * ks + g4) ^ swizzle(l16)) << 4);
+    for (int ks = 0; ks < KS; ++ks) koff[ks] = k0 ^ (ks << 6);
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      const int r = 4 * g4 + (l16 >> 2);
-      vtr[cb] = r * ROWB + (((2 * cb + ((l16 & 3) >> 1)) ^ swizzle(r)) << 4) + (l16 & 1) * 8;
-    }
+    for (int cb = 0; cb < CB; ++cb) vtr[cb] = v0 ^ (cb << 5);
   }
   __device__ void load_q(int nq, const T* row, int g4) {
 #pragma unroll
@@ -104,7 +104,7 @@ struct CoreBf16 {
   // this lane's channels of query column nq, times f, into its row
   __device__ void store(f32x4* row, int nq, float f, int g4, int l16) const {
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) row[(4 * cb + g4) ^ l16] = O[cb][nq] * f;
+    for (int cb = 0; cb < CB; ++cb) row[(g4 ^ l16) ^ (4 * cb)] = O[cb][nq] * f;
   }
 };
 
@@ -117,8 +117,9 @@ struct CoreF32 {
   int koff[KS], voff[4];
   __device__ static int swizzle(int row) { return row & 15; }
   __device__ void init(int l16, int g4) {
+    const int k0 = l16 * ROWB + (((g4 * KS) ^ swizzle(l16)) << 4);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) koff[ks] = l16 * ROWB + (((g4 * KS + ks) ^ swizzle(l16)) << 4);
+    for (int ks = 0; ks < KS; ++ks) koff[ks] = k0 ^ (ks << 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) voff[i] = (4 * g4 + i) * ROWB + ((l16 ^ swizzle(4 * g4 + i)) << 4);
   }
@@ -258,11 +259,12 @@ __global__ __launch_bounds__(THREADS, 1) void paged_rows_kernel(const PagedArgs 
       core.load_q(nq, row, g4);
       least = limit[nq] < least ? limit[nq] : least;
     }
-    // Also where this wavefront has fewer stages (the loads are then empty): the compiler counts what is under way.
-    load(0, B0{});
-    look_up(1);
-    load(1, B1{});
-    if (stages > 2) look_up(2);
+    load(0, B0{});  // empty where this wavefront has no stage: the compiler counts what is under way behind the queries
+    if (stages > 1) {
+      look_up(1);
+      load(1, B1{});
+      if (stages > 2) look_up(2);
+    }
 #pragma unroll
     for (int x = 1; x < 16; x *= 2) {
       const int other = __shfl_xor(least, x);
