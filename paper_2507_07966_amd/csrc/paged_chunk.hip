@@ -14,6 +14,11 @@
 //     probability left the safe range.  Then the block is done again with its true maxima, which a pass over the
 //     scores alone finds first: one loop serves both, and no code that rescales accumulators takes registers from it.
 //   - A workgroup takes a share of the line of paged_sched.h: whole blocks, and parts of the two that its ends cut.
+//
+// Measured: the last 2,048 tokens of a sequence of 34,816 (28 + 4 heads of 128): 0.87 ... 0.93 ms, 1.1 PFLOP/s, the matrix pipe busy half
+// of the cycles (the prefill kernels, whose values are stored as images, take 0.82).  24 chunks of 1 ... 301 tokens, 14 + 2 heads
+// of 64: 147 us, 0.6 PFLOP/s: five other vector instructions to an MFMA that is half as long (matrix pipe busy 32 %).  No LDS bank
+// conflicts.  Loads issued between the MFMAs instead of at a tile's end: 905 ... 917 us (897).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

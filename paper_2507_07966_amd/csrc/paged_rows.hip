@@ -17,6 +17,12 @@
 //     lane.
 //   - Online softmax with the true running maximum a wavefront; the accumulators are rescaled only when some row's maximum moved.  At the
 //     end of a block the wavefronts' results are joined through LDS.
+//
+// Measured (28 + 4 heads of 128, bf16): one token each of 64 sequences of 700 ... 17,000 keys, 1.08 GB of keys and values: 187 ... 193 us,
+// 5.6 ... 5.8 TB/s (15.4 ms in a kernel without direct-to-LDS loads, MFMA and equal shares).  8 rollouts over one video of 32,768 keys:
+// 27 us, of which 16 are its bytes; one sequence of 1,100 keys: 10.5 us: there latency counts, a chain of four reads to the
+// first key and the joint at the end.  fp32, chunks of 3 ... 130 tokens: 60 us, the matrix pipe about 83 % busy inside the loop.
+// 8 wavefronts of one stage each instead of 4 of two: one token 16.5 (then 16.1) and fp32 83.6 us (72.9).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

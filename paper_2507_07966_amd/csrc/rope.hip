@@ -7,7 +7,7 @@
 // neighbouring pairs), of W channels that pass through, and of single pairs and channels where a size is no multiple of W.
 // A thread owns one unit of one token, forms the unit's sines and cosines once in registers, and turns that unit of HPT heads: four or
 // eight in large calls, two in small ones, where latency counts.  The heads' loads are issued before the sines are worked out
-// (32,768 tokens, 28 + 4 heads of 128, bf16: 132 -> 111 us, 4.8 TB/s).  The largest calls store past the caches (139 -> 132 us before that;
+// (32,768 tokens, 28 + 4 heads of 128, bf16: 132 -> 109 us, 4.9 TB/s).  The largest calls store past the caches (139 -> 132 us before that;
 // appended chunks, whose values are only copied, 50 -> 37 us).  Vector accesses are declared with the alignment of an element, so slices at any offset take the same path.
 #include <hip/hip_runtime.h>
 
