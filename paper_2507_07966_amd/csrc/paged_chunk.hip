@@ -15,10 +15,11 @@
 //     scores alone finds first: one loop serves both, and no code that rescales accumulators takes registers from it.
 //   - A workgroup takes a share of the line of paged_sched.h: whole blocks, and parts of the two that its ends cut.
 //
-// Measured: the last 2,048 tokens of a sequence of 34,816 (28 + 4 heads of 128): 0.87 ... 0.93 ms, 1.1 PFLOP/s, the matrix pipe busy half
+// Measured: the last 2,048 tokens of a sequence of 34,816 (28 + 4 heads of 128): 0.87 ... 0.92 ms, 1.1 PFLOP/s, the matrix pipe busy half
 // of the cycles (the prefill kernels, whose values are stored as images, take 0.82).  24 chunks of 1 ... 301 tokens, 14 + 2 heads
-// of 64: 147 us, 0.6 PFLOP/s: five other vector instructions to an MFMA that is half as long (matrix pipe busy 32 %).  No LDS bank
-// conflicts.  Loads issued between the MFMAs instead of at a tile's end: 905 ... 917 us (897).
+// of 64: 132 us, 0.65 PFLOP/s: about five other vector instructions to an MFMA that is half as long (matrix pipe busy a third).  No LDS
+// bank conflicts.  Loads issued between the MFMAs instead of at a tile's end: 905 ... 917 us (897); half of the wavefronts half a tile behind
+// the others, with a buffer more: 902 (874) and 147 (132); wave priorities make no difference.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -80,6 +81,9 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
     const int first_key = seg.key0 + p.tile0 * TILE, tiles = p.tile1 - p.tile0;
 
     // ---- this lane's two query columns
+    // A wavefront without rows only loads: with at most half of a block's rows every SIMD has one wavefront left that computes, and a tile takes
+    // about half the time (a token a sequence in such blocks: 271 -> 203 us, the rate of memory), which the schedule counts on.
+    const bool idle = wave * ROWS_PER_WAVE >= block_rows;
     bf16x8 Q[NQ][KS];
     int limit[NQ];  // last key that column nq sees
 #pragma unroll
@@ -285,9 +289,20 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
       // Step t: the scores of tile t, then the product of tile t - 1 and the softmax of tile t.  Tile t is in buffer t % BUFS; K of
       // tile t + AHEAD goes where K of tile t - 1 was, V of the tile before it where V of tile t - 2 was.
       int buf = 0;  // of tile t - 1
-      for (int t = 1; t < tiles; ++t) {
-        const int old = buf, older = old == 0 ? AHEAD * TILE_BYTES : old - TILE_BYTES;
-        buf = old == AHEAD * TILE_BYTES ? 0 : old + TILE_BYTES;
+      auto after = [&](int b) { return b == AHEAD * TILE_BYTES ? 0 : b + TILE_BYTES; };
+      auto next_tile = [&](int t, int old) {
+        issue_next(t + AHEAD, page, old == 0 ? AHEAD * TILE_BYTES : old - TILE_BYTES, old);
+        page = look_up(t + AHEAD + 1);
+        wait_loads<(AHEAD - 1) * 2 * LOADS>();  // K of tile t + 1 and V of tile t
+        barrier_with_loads();
+      };
+      int t = 1;
+      if (idle) {
+        for (; t < tiles; ++t, buf = after(buf)) next_tile(t, buf);
+      }
+      for (; t < tiles; ++t) {
+        const int old = buf;
+        buf = after(old);
         scores(smem + buf);
         mask(t);
         bf16x8 Pn[2][NQ];
@@ -296,10 +311,7 @@ __global__ __launch_bounds__(THREADS, 1) void paged_chunk_kernel(const PagedArgs
         for (int nq = 0; nq < NQ; ++nq) lacc[nq] = 0.f;
         product(smem + VBUF + old, std::true_type{}, Pn, lacc);
         accept(Pn, lacc);
-        issue_next(t + AHEAD, page, older, old);
-        page = look_up(t + AHEAD + 1);
-        wait_loads<(AHEAD - 1) * 2 * LOADS>();  // K of tile t + 1 and V of tile t
-        barrier_with_loads();
+        next_tile(t, old);
       }
       {
         bf16x8 Pn[2][NQ];

@@ -4,9 +4,9 @@
 //
 // The work is a line.  A SEGMENT is a sequence with its new rows (and, with shared pages, one more for the shared
 // keys, whose rows are those of all sequences); segments follow each other, in a segment the kv heads, in a head the blocks
-// of `block_rows` stacked rows m = i * group + (h % group).  A block costs its keys plus what starting and ending it costs; the
-// line is cut into equal shares, one a workgroup, and a block that a cut falls into becomes PIECES over
-// disjoint ranges of its key tiles, whose partial results are merged.  Cutting by length on the device is what makes
+// of `block_rows` stacked rows m = i * group + (h % group).  A block costs its keys (half of them where a sequence has so few rows that half
+// of the workgroup idles) plus what starting and ending it costs; the line is cut into equal shares, one a workgroup, and a block that a
+// cut falls into becomes PIECES over disjoint ranges of its key tiles, whose partial results are merged.  Cutting by length on the device is what makes
 // one launch fit all lengths: a call with one long sequence and many short ones keeps every compute unit busy to the end.
 //
 // Before its first load a workgroup can do nothing else than this, so it is kept short: cost is counted in units of
@@ -33,6 +33,7 @@ struct PagedShape {
   int32_t start_cost;   // of a block beside its keys, in units
   int32_t more_cost;    // by how much a block of new tokens costs more than the one before it: its tokens
   int32_t min_share;    // units: a smaller share is not worth a workgroup and a merge
+  int32_t half_rows;    // a sequence of at most so many rows has a block of half the cost a key
   int32_t causal_cuts;  // cuts keep out of the tiles whose first key some row of the block does not see
   float per_group;      // a little more than 1 / workgroups
   float inv_group;      // 1 / group
@@ -70,6 +71,10 @@ PA_HD int32_t div_small(int32_t a, int32_t b) {
 // x / group for 0 <= x < 2^20: half a step away from the next integer, fp32 rounding does not matter
 PA_HD int32_t group_of(const PagedShape& s, int32_t x) { return (int32_t)(((float)x + 0.5f) * s.inv_group); }
 
+// log2 of the keys that cost a unit in this segment
+PA_HD int32_t key_shift_of(const PagedShape& s, const Segment& g) {
+  return s.unit_shift + ((uint32_t)g.tokens * (uint32_t)s.group <= (uint32_t)s.half_rows);
+}
 PA_HD Segment make_segment(const PagedShape& s, int32_t token0, int32_t tokens, int32_t first_pos, int32_t key0, int32_t keys, int32_t more) {
   Segment g;
   g.token0 = token0;
@@ -78,7 +83,7 @@ PA_HD Segment make_segment(const PagedShape& s, int32_t token0, int32_t tokens, 
   const uint32_t rows = (uint32_t)tokens * (uint32_t)s.group;
   g.blocks = rows <= (uint32_t)s.block_rows ? (rows > 0) : (int32_t)((rows + s.block_rows - 1) / (uint32_t)s.block_rows);
   g.first_pos = first_pos;
-  g.first_cost = s.start_cost + (keys >> s.unit_shift);
+  g.first_cost = s.start_cost + (keys >> key_shift_of(s, g));
   g.more_cost = more;
   g.cost = blocks_cost(g, g.blocks);
   return g;
@@ -136,7 +141,7 @@ PA_HD Piece make_piece(const PagedShape& s, const Segment& g, bool shared, const
   p.tile0 = 0;
   p.tile1 = tiles;
   if (!p.whole) {
-    const int32_t shift = s.unit_shift - s.tile_shift;
+    const int32_t shift = key_shift_of(s, g) - s.tile_shift;
     auto tile = [&](int32_t x) {
       const int64_t u = x - b.c0 - s.start_cost;
       const int64_t t = u <= 0 ? 0 : shift >= 0 ? u << shift : u >> -shift;

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.sampling_util import Paged, gpu, host
+from tests.sampling_util import Paged, gpu, host, round_to
 
 pytestmark = pytest.mark.gpu
 
@@ -44,6 +44,22 @@ def test_attention_is_the_definition(name):
     if shared:
         x.check(*x.attend(shared_len=shared + page // 2), want)   # rounded down to whole pages
         x.check(*x.attend(shared_len=page), want)
+
+
+@pytest.mark.parametrize("heads,dim,page,lens,new", [((28, 4), 128, 64, [900, 2500, 70, 1300, 4100], [1, 400, 18, 1, 19]),
+                                                     ((14, 2), 64, 32, [3000, 700, 900, 5000, 33], [1, 300, 1, 9, 2])])
+@pytest.mark.parametrize("late", [False, True])
+def test_tokens_beside_a_chunk(heads, dim, page, lens, new, late):
+    """Blocks of few rows, in which some wavefronts have none, in a call of chunks; `late`: with scores of hundreds, the largest last."""
+    x = Paged("bf16", heads, dim, page, lens, new, pad=3, seed=30 + late)
+    if late:
+        grow = np.zeros((x.pages, 1, x.page, 1))
+        for b, n in enumerate(x.lens):
+            for j in range(n):
+                grow[x.table[b, j // x.page], 0, j % x.page, 0] = 8.0 * j / n
+        x.k = round_to(x.k * grow, "bf16")
+        x.q = round_to(x.q * 4.0, "bf16")
+    x.check(*x.attend())
 
 
 @pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("bf16", 64), ("f32", 128)])

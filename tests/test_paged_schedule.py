@@ -52,6 +52,8 @@ CASES = [
     ("bf16", (14, 2), 64, [400, 9000, 0, 77, 5000], [300, 1, 0, 77, 200], -1), ("f32", (8, 2), 128, [200, 4100, 3000], [130, 3, 77], -1),
     ("f32", (4, 4), 64, [400, 350, 321], [1, 2, 1], 320), ("bf16", (40, 1), 128, [300, 77], [1, 1], -1), ("bf16", (600, 1), 64, [900, 12], [3, 12], -1),
     ("bf16", (28, 4), 128, [50, 3, 20], [70, 3, 30], -1), ("bf16", (8, 8), 128, [38400, 39000], [1, 1], -1), ("bf16", (8, 2), 128, [100, 700], [1, 1], 64),
+    ("bf16", (28, 4), 128, [9000, 7000, 3100, 8200, 40, 6000], [1, 18, 900, 19, 1, 400], -1),   # blocks of half the cost beside whole ones
+    ("bf16", (14, 2), 64, [9000 + 17 * i for i in range(30)], [2000] + [1] * 29, -1),
 ]
 
 
