@@ -15,9 +15,9 @@
 //     scores alone finds first: one loop serves both, and no code that rescales accumulators takes registers from it.
 //   - A workgroup takes a share of the line of paged_sched.h: whole blocks, and parts of the two that its ends cut.
 //
-// Measured: the last 2,048 tokens of a sequence of 34,816 (28 + 4 heads of 128): 0.87 ... 0.92 ms, 1.1 PFLOP/s, the matrix pipe busy half
+// Measured: the last 2,048 tokens of a sequence of 34,816 (28 + 4 heads of 128): 0.87 ... 0.92 ms, 1.1 PFLOP/s, the matrix pipe busy 54 %
 // of the cycles (the prefill kernels, whose values are stored as images, take 0.82).  24 chunks of 1 ... 301 tokens, 14 + 2 heads
-// of 64: 132 us, 0.65 PFLOP/s: about five other vector instructions to an MFMA that is half as long (matrix pipe busy a third).  No LDS
+// of 64: 132 us, 0.65 PFLOP/s: 4.6 other vector instructions to an MFMA that is half as long (matrix pipe busy 30 %).  No LDS
 // bank conflicts.  Loads issued between the MFMAs instead of at a tile's end: 905 ... 917 us (897); half of the wavefronts half a tile behind
 // the others, with a buffer more: 902 (874) and 147 (132); wave priorities make no difference.
 #include <hip/hip_runtime.h>

@@ -6,8 +6,8 @@
 // keys, whose rows are those of all sequences); segments follow each other, in a segment the kv heads, in a head the blocks
 // of `block_rows` stacked rows m = i * group + (h % group).  A block costs its keys (half of them where a sequence has so few rows that half
 // of the workgroup idles) plus what starting and ending it costs; the line is cut into equal shares, one a workgroup, and a block that a
-// cut falls into becomes PIECES over disjoint ranges of its key tiles, whose partial results are merged.  Cutting by length on the device is what makes
-// one launch fit all lengths: a call with one long sequence and many short ones keeps every compute unit busy to the end.
+// cut falls into becomes PIECES over disjoint ranges of its key tiles, whose partial results are merged.  Cutting by length on the device
+// is what makes one launch fit all lengths: a call with one long sequence and many short ones keeps every compute unit busy to the end.
 //
 // Before its first load a workgroup can do nothing else than this, so it is kept short: cost is counted in units of
 // 2^unit_shift keys, which the host chooses such that no call of its sizes exceeds 2^30 units (16 keys, but for calls beyond any real
