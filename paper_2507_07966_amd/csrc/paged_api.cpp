@@ -210,7 +210,7 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   while (most / (double)((int64_t)1 << s.unit_shift) > (double)(1 << 29)) ++s.unit_shift;
   s.start_cost = (costs.start_keys >> s.unit_shift) + 1;
   s.min_share = (costs.min_share >> s.unit_shift) + 1;
-  s.more_cost = (s.block_rows / s.group) >> s.unit_shift;
+  s.growth = (s.block_rows << pa::GROWTH_SHIFT) / s.group;
   s.per_group = (1.0f + 1.0f / (1 << 20)) / (float)a.groups;
   if (!ws) return a;  // the schedule alone
   a.line = reinterpret_cast<pa::PagedLine*>(ws);
@@ -380,7 +380,7 @@ int64_t paged_attn_schedule(const paged_attn_plan_t* plan, const int32_t* seq_le
         continue;
       }
       const bool shared = with && i == 0;
-      const int32_t head = pa::div_small(x - start, g.cost), head_start = start + head * g.cost, block = pa::block_at(g, x - head_start);
+      const int32_t head = pa::div_small(x - start, g.cost), head_start = start + head * g.cost, block = pa::block_at(s, g, x - head_start);
       const pa::Block b = pa::make_block(s, g, head_start, block);
       const pa::Piece p = pa::make_piece(s, g, shared, b, x, end);
       if (count < max_pieces) {

@@ -272,12 +272,12 @@ __device__ inline bool begin_walk(const PagedArgs& a, Walk& w) {
   w.seg.blocks = __builtin_amdgcn_readfirstlane(found.blocks);
   w.seg.first_pos = __builtin_amdgcn_readfirstlane(found.first_pos);
   w.seg.first_cost = __builtin_amdgcn_readfirstlane(found.first_cost);
-  w.seg.more_cost = __builtin_amdgcn_readfirstlane(found.more_cost);
+  w.seg.growth = __builtin_amdgcn_readfirstlane(found.growth);
   w.seg.cost = __builtin_amdgcn_readfirstlane(found.cost);
   const int32_t seg_start = __builtin_amdgcn_readfirstlane((int32_t)found_start);
   w.head = __builtin_amdgcn_readfirstlane(div_small(w.x - seg_start, w.seg.cost));
   w.head_start = seg_start + w.head * w.seg.cost;
-  w.block_index = __builtin_amdgcn_readfirstlane(block_at(w.seg, w.x - w.head_start));
+  w.block_index = __builtin_amdgcn_readfirstlane(block_at(w.shape, w.seg, w.x - w.head_start));
   w.enter(a);
   if (tid == 0) a.cuts[w.position] = PagedCut{0, 0, 0, 0, 0, 0};
   return true;

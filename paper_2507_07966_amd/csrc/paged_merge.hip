@@ -165,7 +165,7 @@ __global__ __launch_bounds__(THREADS) void merge_rows_kernel(const PagedArgs a) 
   auto pieces = [&](const Segment& g, int32_t start, bool shared) {
     const uint32_t m = (uint32_t)(t - g.token0) * s.group + j;
     const int block = (int)(m / (uint32_t)s.block_rows), r = (int)(m - (uint32_t)block * s.block_rows);
-    const int32_t c0 = start + head * g.cost + blocks_cost(g, block), c1 = c0 + g.first_cost + block * g.more_cost;
+    const int32_t head_start = start + head * g.cost, c0 = head_start + blocks_cost(s, g, block), c1 = head_start + blocks_cost(s, g, block + 1);
     const int32_t first = div_small(c0, share), last = div_small(c1 - 1, share);
     if (first == last) return Pieces{1, ((shared ? (int64_t)s.T : 0) + t) * a.Hq + h, true, first, r};
     return Pieces{last - first + 1, (2 * (int64_t)first + 1) * s.block_rows + r, false, first, r};

@@ -31,7 +31,7 @@ struct PagedShape {
   int32_t shared;       // leading keys of all sequences that form a segment of their own (whole pages); 0: none
   int32_t unit_shift;
   int32_t start_cost;   // of a block beside its keys, in units
-  int32_t more_cost;    // by how much a block of new tokens costs more than the one before it: its tokens
+  int32_t growth;       // by how many keys a block of new tokens sees more than the one before it (a block's tokens), times 2^GROWTH_SHIFT
   int32_t min_share;    // units: a smaller share is not worth a workgroup and a merge
   int32_t half_rows;    // a sequence of at most so many rows has a block of half the cost a key
   int32_t causal_cuts;  // cuts keep out of the tiles whose first key some row of the block does not see
@@ -39,12 +39,18 @@ struct PagedShape {
   float inv_group;      // 1 / group
 };
 
+// A block's tokens, block_rows / group, are no whole number, and in a prefill from nothing the new tokens are most of the keys, so the growth
+// is not rounded before it is summed: in units of 16 keys it was 32 for 36.6 tokens and 0 for 12.8, and the fullest share of 4,096 tokens from
+// nothing had 2.95 (32 + 1 heads, bf16) and 2.38 (8 + 2, fp32) times the mean of the tiles; now 1.11 and 1.05 (355 -> 185 us; 2,048
+// tokens of 8 + 2 heads in fp32: 244 -> 123).
+constexpr int GROWTH_SHIFT = 12;
+
 struct Segment {
   int32_t token0, tokens;  // packed rows
   int32_t key0;            // first key
   int32_t blocks;          // of one kv head
   int32_t first_pos;       // position of the first token
-  int32_t first_cost, more_cost;  // of block 0, and by how much each next one costs more
+  int32_t first_cost, growth;  // cost of block 0; as in PagedShape, 0 for the shared keys
   int32_t cost;            // of one kv head; -1: cu_new falls here, and the call does nothing
 };
 
@@ -55,8 +61,9 @@ struct Piece {
 };
 
 PA_HD int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
-PA_HD int32_t blocks_cost(const Segment& g, int32_t n) {
-  return n * g.first_cost + (g.more_cost ? (int32_t)((int64_t)n * (n - 1) / 2 * g.more_cost) : 0);
+// Of a head's first n blocks.  (n * growth is below 2^37, as a sequence has at most 2^24 tokens, and n below 2^27: 2^63 is not reached.)
+PA_HD int32_t blocks_cost(const PagedShape& s, const Segment& g, int32_t n) {
+  return n * g.first_cost + (n > 1 ? (int32_t)((int64_t)n * (n - 1) / 2 * g.growth >> (GROWTH_SHIFT + s.unit_shift)) : 0);
 }
 // a / b for 0 <= a < 2^31, b > 0 and a quotient below 2^20: guessed in fp32, off by at most one, and put right
 PA_HD int32_t div_small(int32_t a, int32_t b) {
@@ -75,7 +82,7 @@ PA_HD int32_t group_of(const PagedShape& s, int32_t x) { return (int32_t)(((floa
 PA_HD int32_t key_shift_of(const PagedShape& s, const Segment& g) {
   return s.unit_shift + ((uint32_t)g.tokens * (uint32_t)s.group <= (uint32_t)s.half_rows);
 }
-PA_HD Segment make_segment(const PagedShape& s, int32_t token0, int32_t tokens, int32_t first_pos, int32_t key0, int32_t keys, int32_t more) {
+PA_HD Segment make_segment(const PagedShape& s, int32_t token0, int32_t tokens, int32_t first_pos, int32_t key0, int32_t keys, int32_t growth) {
   Segment g;
   g.token0 = token0;
   g.tokens = tokens;
@@ -84,8 +91,8 @@ PA_HD Segment make_segment(const PagedShape& s, int32_t token0, int32_t tokens, 
   g.blocks = rows <= (uint32_t)s.block_rows ? (rows > 0) : (int32_t)((rows + s.block_rows - 1) / (uint32_t)s.block_rows);
   g.first_pos = first_pos;
   g.first_cost = s.start_cost + (keys >> key_shift_of(s, g));
-  g.more_cost = more;
-  g.cost = blocks_cost(g, g.blocks);
+  g.growth = growth;
+  g.cost = blocks_cost(s, g, g.blocks);
   return g;
 }
 // Sequence b's new rows and its own keys; cu0, cu1 = cu_new[b], cu_new[b + 1], len = seq_lens[b], whatever they hold.  (A first position
@@ -93,8 +100,9 @@ PA_HD Segment make_segment(const PagedShape& s, int32_t token0, int32_t tokens, 
 PA_HD Segment own_segment(const PagedShape& s, int32_t cu0, int32_t cu1, int32_t len) {
   const int32_t lo = (int32_t)clamp64(cu0, 0, s.T), hi = (int32_t)clamp64(cu1, 0, s.T);
   const int32_t first = (int32_t)clamp64((int64_t)len - cu1 + lo, -(1 << 30), s.capacity);
-  const int32_t before = first - s.shared;
-  Segment g = make_segment(s, lo, hi > lo ? hi - lo : 0, first, s.shared, before > 0 ? before : 0, s.more_cost);
+  const int32_t tokens = hi > lo ? hi - lo : 0, of_block = (s.growth + (1 << GROWTH_SHIFT) - 1) >> GROWTH_SHIFT;
+  const int32_t keys = first + (tokens < of_block ? tokens : of_block) - s.shared;  // that block 0 sees
+  Segment g = make_segment(s, lo, tokens, first, s.shared, keys > 0 ? keys : 0, s.growth);
   if (cu1 < cu0) g.cost = -1;  // sequences might overlap, and the line be longer than the unit allows for
   return g;
 }
@@ -113,8 +121,8 @@ struct Block {
 };
 PA_HD Block make_block(const PagedShape& s, const Segment& g, int32_t head_start, int32_t block) {
   Block b;
-  b.c0 = head_start + blocks_cost(g, block);
-  b.c1 = b.c0 + g.first_cost + block * g.more_cost;
+  b.c0 = head_start + blocks_cost(s, g, block);
+  b.c1 = head_start + blocks_cost(s, g, block + 1);
   const uint32_t row0 = (uint32_t)block * (uint32_t)s.block_rows, left = (uint32_t)g.tokens * (uint32_t)s.group - row0;
   b.rows = left < (uint32_t)s.block_rows ? (int32_t)left : s.block_rows;
   b.token = block ? (int32_t)(row0 / (uint32_t)s.group) : 0;
@@ -153,13 +161,13 @@ PA_HD Piece make_piece(const PagedShape& s, const Segment& g, bool shared, const
   return p;
 }
 // The block of a kv head in which cost `rem` of that head lies.
-PA_HD int32_t block_at(const Segment& g, int32_t rem) {
+PA_HD int32_t block_at(const PagedShape& s, const Segment& g, int32_t rem) {
   if (g.blocks <= 1) return 0;
-  if (g.more_cost == 0) return (int32_t)((uint32_t)rem / (uint32_t)g.first_cost);
+  if (g.growth == 0) return (int32_t)((uint32_t)rem / (uint32_t)g.first_cost);
   int32_t lo = 0, hi = g.blocks - 1;
   while (lo < hi) {
     const int32_t mid = (lo + hi + 1) >> 1;
-    if (blocks_cost(g, mid) <= rem) lo = mid; else hi = mid - 1;
+    if (blocks_cost(s, g, mid) <= rem) lo = mid; else hi = mid - 1;
   }
   return lo;
 }

@@ -1,0 +1,31 @@
+"""The shares of paged_attn_forward's workgroups are alike, by the tiles of keys that they load, also where the new tokens themselves are most of the keys:
+fp32 and wide groups, whose blocks have few tokens, prefills from nothing, and chunks of several lengths."""
+import numpy as np
+import pytest
+
+import paper_2507_07966_amd as pa
+
+CALLS = [
+    ("f32", (8, 2), 128, [2100], [2048]), ("f32", (28, 4), 128, [1300], [1200]), ("f32", (14, 2), 64, [2000], [1900]),
+    ("f32", (8, 2), 128, [4096], [4096]), ("f32", (32, 1), 128, [2048], [2048]), ("f32", (8, 8), 64, [2900, 700], [2900, 650]),
+    ("bf16", (32, 1), 128, [4096], [4096]), ("bf16", (40, 1), 128, [4096], [4096]), ("bf16", (28, 4), 128, [8192], [8192]),
+    ("bf16", (300, 1), 64, [2999], [2999]), ("bf16", (14, 2), 64, [3000, 900, 77, 4000], [3000, 900, 77, 4000]),
+    ("bf16", (28, 4), 128, [34816], [2048]),
+]
+
+
+@pytest.mark.parametrize("dtype,heads,dim,lens,new", CALLS, ids=lambda v: "-".join(map(str, v)) if isinstance(v, (tuple, list)) else str(v))
+def test_shares_of_prefills_are_balanced(dtype, heads, dim, lens, new):
+    tokens, page = sum(new), 64
+    p = pa.paged_attn_plan(*heads, dim, page, 100000, -(-max(lens) // page), len(lens), tokens, 0.1, dtype=dtype, device=-1)
+    groups, _, tile = p.schedule_shape(len(lens), tokens)
+    pieces = p.schedule(lens, np.concatenate([[0], np.cumsum(new)]), tokens)
+    p.destroy()
+    tiles = np.maximum(0, -(-(pieces[:, 6] - pieces[:, 5]) // tile))
+    load = np.bincount(pieces[:, 0], weights=tiles, minlength=groups)
+    # A share of w keys' cost has at most w / tile tiles and one more for each end that rounding moves.  It holds that many where it starts no block, and by
+    # up to 384 keys (start_keys of the chunks, the larger) fewer for each block that it starts: 384 / tile above the mean, where that mean is of shares
+    # that start one each.  15 % for what is not worth counting: blocks' last, partly visible tiles.
+    most = 1.15 * load.mean() + 384 / tile + 2
+    print(f"most {load.max():.0f} of a mean of {load.mean():.1f}, bound {most:.1f}")
+    assert load.max() <= most
