@@ -145,7 +145,15 @@ class PagedAttnPlan:
         """The pieces of work that paged_attn_forward's workgroups take for these lengths (host arrays; shared_len -1: not given): int32
         [n, 8] = (share, sequence (-1: the shared keys), kv head, first stacked row, rows, first key, end of the keys, whole block)."""
         lib = _lib or _load()
-        lens, cu = np.ascontiguousarray(seq_lens, dtype=np.int32), np.ascontiguousarray(cu_new, dtype=np.int32)
+        lens, cu = np.asarray(seq_lens), np.asarray(cu_new)
+        if lens.ndim != 1 or cu.shape != (len(lens) + 1,):   # the library reads so many of them
+            _refuse(_SHAPE, "schedule", f"seq_lens [n] and cu_new [n + 1], not {list(lens.shape)} and {list(cu.shape)}")
+        for name, x in (("seq_lens", lens), ("cu_new", cu), ("num_tokens", np.asarray(num_tokens)), ("shared_len", np.asarray(shared_len))):
+            if x.dtype.kind not in "iu" and x.size:
+                _refuse(_UNSUPPORTED, "schedule", f"{name} has to be whole numbers, not {x.dtype}")
+            if x.size and not -(1 << 31) <= int(x.min()) <= int(x.max()) < 1 << 31:
+                _refuse(_SHAPE, "schedule", f"{name} does not fit 32 bits")
+        lens, cu = (np.ascontiguousarray(x, dtype=np.int32) for x in (lens, cu))
         args = self.handle, lens.ctypes.data, cu.ctypes.data, len(lens), int(num_tokens), int(shared_len)
         n = lib.paged_attn_schedule(*args, None, 0)
         if n < 0:

@@ -1,5 +1,5 @@
-"""The shares of paged_attn_forward's workgroups are alike, by the tiles of keys that they load, also where the new tokens themselves are most of the keys:
-fp32 and wide groups, whose blocks have few tokens, prefills from nothing, and chunks of several lengths."""
+"""The division of paged_attn_forward among workgroups: shares are alike, by the tiles of keys that they load, also where the new tokens themselves are most of the
+keys (fp32 and wide groups, whose blocks have few tokens, prefills from nothing, chunks of several lengths), and what PagedAttnPlan.schedule refuses."""
 import numpy as np
 import pytest
 
@@ -29,3 +29,18 @@ def test_shares_of_prefills_are_balanced(dtype, heads, dim, lens, new):
     most = 1.15 * load.mean() + 384 / tile + 2
     print(f"most {load.max():.0f} of a mean of {load.mean():.1f}, bound {most:.1f}")
     assert load.max() <= most
+
+
+@pytest.mark.parametrize("lens,cu,tokens,shared,status", [
+    ([50, 60], [0, 1], 2, -1, 2), ([50, 60], [0], 2, -1, 2), ([50], [0, 1, 2], 2, -1, 2), ([50], 1, 1, -1, 2), ([[50]], [[0, 1]], 1, -1, 2),
+    ([], [], 1, -1, 2), ([1 << 32], [0, 1], 1, -1, 2), ([50], [0, 1 << 31], 1, -1, 2), ([50], [0, 1], 1 << 64, -1, 3), ([50], [0, 1], 1 << 33, -1, 2),
+    ([50], [0, 1], 1, 1 << 32, 2), ([50.5], [0, 1], 1, -1, 3), ([50], [0, 1], 1.0, -1, 3),
+])
+def test_schedule_refuses_arrays_that_do_not_fit(lens, cu, tokens, shared, status):
+    """The library reads n lengths and n + 1 ends: shorter arrays were read beyond their end, and wider numbers wrapped."""
+    p = pa.paged_attn_plan(4, 2, 64, 16, 100, 8, 8, 64, 0.1, device=-1)
+    with pytest.raises(pa.PrefixAttnError) as e:
+        p.schedule(lens, cu, tokens, shared)
+    assert e.value.status == status
+    assert len(p.schedule(np.array([50, 7]), np.array([0, 1, 2]), 2)) > 0
+    p.destroy()
