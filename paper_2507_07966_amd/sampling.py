@@ -109,7 +109,7 @@ def rope_axes(sections: Sequence[int], head_dim: int, rotary_dim: Optional[int] 
         axes = [a for a, n in enumerate(sections) for _ in range(n)]
     d = _RopeDesc()
     d.head_dim, d.rotary_dim, d.layout, d.num_axes = int(head_dim), rotary_dim, LAYOUTS[layout], len(sections)
-    if not 2 <= rotary_dim <= d.head_dim <= 2 * MAX_PAIRS:
+    if not 2 <= rotary_dim <= int(head_dim) <= 2 * MAX_PAIRS:
         _refuse(_SHAPE, "rope_axes", f"rotary_dim {rotary_dim} of head_dim {head_dim}: 2 <= rotary_dim <= head_dim <= {2 * MAX_PAIRS}")
     d.pair_axis[:len(axes)] = axes
     return RopeAxes(d)
@@ -164,6 +164,8 @@ class PagedAttnPlan:
 
     def schedule_shape(self, num_seqs: int, num_tokens: int, shared: bool = False):
         """Workgroups of such a call, rows of a block and keys of a tile."""
+        if not (0 < num_seqs <= self.max_seqs and 0 < num_tokens <= self.max_tokens):
+            _refuse(_SHAPE, "schedule_shape", f"{num_seqs} sequences and {num_tokens} tokens: 1 to {self.max_seqs} and {self.max_tokens} on this plan")
         v = [ctypes.c_int32() for _ in range(3)]
         st = (_lib or _load()).paged_attn_schedule_shape(self.handle, int(num_seqs), int(num_tokens), int(shared), *map(ctypes.byref, v))
         if st:

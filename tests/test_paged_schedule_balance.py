@@ -44,3 +44,16 @@ def test_schedule_refuses_arrays_that_do_not_fit(lens, cu, tokens, shared, statu
     assert e.value.status == status
     assert len(p.schedule(np.array([50, 7]), np.array([0, 1, 2]), 2)) > 0
     p.destroy()
+
+
+def test_numbers_beyond_32_bits_do_not_wrap():
+    for head_dim in ((1 << 32) + 64, (1 << 64) + 64, 64 - (1 << 32)):   # each is 64 in 32 bits
+        with pytest.raises(pa.PrefixAttnError):
+            pa.rope_axes((32,), head_dim, rotary_dim=64)
+    p = pa.paged_attn_plan(4, 2, 64, 16, 100, 8, 8, 64, 0.1, device=-1)
+    for seqs, tokens in (((1 << 32) + 1, 1), (1, (1 << 64) + 1), (9, 1), (1, 65), (0, 1), (1, 0)):
+        with pytest.raises(pa.PrefixAttnError) as e:
+            p.schedule_shape(seqs, tokens)
+        assert e.value.status == 2
+    assert p.schedule_shape(8, 64) and p.schedule_shape(1, 1)
+    p.destroy()
