@@ -1,6 +1,7 @@
-"""Build libprefix_attn.so (C-ABI library, gfx950) in-tree with hipcc.
+"""Build libprefix_attn.so (C-ABI library, gfx950) in-tree with hipcc, and beside it _sampling.so, the Python module of the sampling calls, with g++.
 
-Run `python -m paper_2507_07966_amd.build`.  hipcc cross-compiles without a GPU.
+Run `python -m paper_2507_07966_amd.build`.  hipcc cross-compiles without a GPU.  The library needs nothing but hipcc: where torch or Python's headers are
+missing it is built alone, for programs that use the C ABI.
 """
 from __future__ import annotations
 
@@ -45,10 +46,15 @@ BINDING = os.path.join(HERE, "_sampling.so")
 
 def binding_commands(bdir: str):
     """Compile and link commands of csrc/py_sampling.cpp, the Python module that checks the sampling calls' tensors: plain C++ against
-    torch's and Python's headers, linked to the library beside it."""
+    torch's and Python's headers, linked to the library beside it.  None where there is no torch or no Python.h."""
     import sysconfig
-    import torch
-    base = os.path.join(os.path.dirname(torch.__file__))
+    try:
+        import torch
+    except ImportError:
+        return None
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return None
+    base = os.path.dirname(torch.__file__)
     obj, lib = os.path.join(bdir, "py_sampling.cpp.o"), os.path.join(base, "lib")
     cc = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
     compile_cmd = [*cc, "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
@@ -75,9 +81,13 @@ def build(verbose: bool = False, extra_flags=(), out: str = LIB) -> str:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
-    if out == LIB:   # other outputs are builds of the library alone
-        compile_cmd, link_cmd = binding_commands(bdir)
-        procs.append(("py_sampling.cpp", subprocess.Popen(compile_cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    # The module's compilation runs beside the library's, which is linked whatever becomes of it.  Other outputs are builds of the library alone.
+    commands, module = binding_commands(bdir) if out == LIB else None, None
+    if commands:
+        try:
+            module = subprocess.Popen(commands[0], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        except OSError as e:
+            module = e
     failed = False
     for src, p in procs:
         log, _ = p.communicate()
@@ -87,12 +97,24 @@ def build(verbose: bool = False, extra_flags=(), out: str = LIB) -> str:
             print(f"[build] {src} FAILED\n{log}", file=sys.stderr)
         elif log.strip() and verbose:
             print(log)
+    log = module.communicate()[0] if isinstance(module, subprocess.Popen) else str(module)
     if failed:
         raise RuntimeError("hipcc failed")
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", out]
     subprocess.run(cmd, check=True)
-    if out == LIB:
-        subprocess.run(link_cmd, check=True)
+    if out != LIB:
+        return out
+    if os.path.exists(BINDING):
+        os.remove(BINDING)   # one of an earlier build must not be taken for this one's
+    if not commands:
+        print(f"[build] no torch or no Python.h here: {os.path.basename(LIB)} alone, without the Python module of the sampling calls", file=sys.stderr)
+        return out
+    if not isinstance(module, subprocess.Popen) or module.returncode != 0:
+        print(f"[build] py_sampling.cpp FAILED\n{log}", file=sys.stderr)
+        raise RuntimeError(f"{commands[0][0]} failed on py_sampling.cpp (the library itself is built: {out})")
+    if verbose and log.strip():
+        print(log)
+    subprocess.run(commands[1], check=True)
     return out
 
 

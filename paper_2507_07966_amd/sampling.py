@@ -57,7 +57,11 @@ def _load_native():
     """Imports the module that checks the calls' tensors; raises if it has not been built (python -m paper_2507_07966_amd.build)."""
     global _native
     _load()   # torch and the library first: the module links to both
-    from . import _sampling
+    try:
+        from . import _sampling
+    except ImportError as e:
+        raise ImportError(f"the module of the sampling calls cannot be loaded ({e}): build it with `python -m paper_2507_07966_amd.build`, which needs "
+                          f"torch, Python's headers and g++") from e
     _native = _sampling
     return _native
 
