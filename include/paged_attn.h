@@ -51,8 +51,8 @@ typedef struct {
  *             overlap it otherwise.  Any alignment of whole elements.
  *   k, k_out  [num_tokens, num_k_heads, D]   likewise, with num_k_heads = 0 and NULL when there are none
  *   positions [num_axes, num_tokens] int32, any sign;  inv_freq [rotary_dim / 2] fp32 (radians per position)
- * num_tokens = 0 is valid and enqueues nothing.  The angle is formed in 64 bits: it stays exact to fp32 for
- * positions of any size. */
+ * num_tokens = 0 is valid and enqueues nothing.  The angle is exact until whole turns are off: sine
+ * and cosine err by at most 4 units of 2^-24 at any position (angles up to 2^51 radians). */
 int rope_axes_forward(const rope_axes_desc_t* desc, int32_t dtype, const void* q, int64_t q_stride, const void* k,
                       int64_t k_stride, int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads,
                       const int32_t* positions, const float* inv_freq, void* q_out, int64_t q_out_stride, void* k_out,
