@@ -116,9 +116,11 @@ int paged_kv_append_rope(const paged_attn_plan_t* plan, const rope_axes_desc_t* 
  *   out        [num_tokens, Hq, D] contiguous, of the plan's dtype
  *   lse_out    [Hq, num_tokens] fp32, or NULL
  *   shared_len NULL, or DEVICE int32: the first *shared_len tokens of every sequence with new tokens (rounded down to whole
- *              pages) are stored in the same pages, named by all their tables, and precede all new tokens.  Calls
- *              of few rows then read those pages once for all sequences: the video of G rollouts.  The result
- *              is that of the call without it; where the tables differ, it is unspecified.
+ *              pages) are stored in the same pages, named by all their tables, and precede all new tokens: the
+ *              video of G rollouts.  Calls of at most 56 rows a sequence on average (a token has Hq / Hkv rows)
+ *              then read those pages once for every 64 rows (fp32: 32) that all sequences have together, instead of once for
+ *              every sequence; other calls do not use it.  The result is that of the call without it; where the tables
+ *              differ, it is unspecified.
  *   workspace  at least the planned size, 16-byte aligned; calls that may overlap need workspaces of their own
  * A row without a visible key (a position below 0) gets zeros and an LSE of minus infinity.  A row that sees a key without a
  * page (an entry outside [0, num_pages), a length beyond the table) gets NaN.  Keys and values that

@@ -147,8 +147,18 @@ int append_call(const paged_attn_plan_t* plan, const rope_axes_desc_t* rope, con
 // Rows of a block for an average of `rows` rows a sequence (with shared keys: rows in all, which their blocks hold together).
 int32_t blocks16_for(int64_t rows, int32_t dtype) { return rows <= 16 ? 1 : rows <= 32 || dtype == PA_F32 ? 2 : 4; }
 
-// A call of at most this many rows a sequence is one of few rows: only such calls use shared_len.
+// A bf16 call of at most this many rows a sequence, on average, is one of few rows.  Measured with either kernel for all calls, few rows and chunks (16
+// sequences of 2,000 ... 6,000 keys, 28 + 4 heads of 128): 14 rows 34 and 44 us, 56 rows 44 and 47, 63 rows 47 and 48, 70 rows 53 and 50,
+// 126 rows 59 and 55, 252 rows 93 and 76; 32 sequences of 4 + 4 heads: 64 rows 64 and 66, 80 rows 92 and 71; 24 of 14 + 2 heads of 64: 63 rows
+// 33 and 37, 126 rows 39 and 40, 252 rows 54 and 50.  The average says little where single tokens run beside one long chunk: 127 of them and
+// a chunk of 1,000 (61.6 rows) take 245 us, 165 in the other kernel, 64 and 512 (62 rows) 294 and 249.
 constexpr int64_t FEW_ROWS = 64;
+// Up to this many rows a sequence, on average, shared keys are a segment of their own.  They save passes over these keys while the blocks
+// of one sequence's rows are not nearly full, and cost a piece more of every row.  With and without, 4, 8, 16 and 64 sequences over 32,768 shared keys, 28 + 4
+// heads of 128: 7 rows 31 and 53, 34 and 91, 49 and 165, 126 and 512 us; 35 rows 52 and 72, 80 and 104, 135 and 179, 418 and 583; 56 rows 64 and 80,
+// 112 and 109, 183 and 183, 691 and 582; 63 rows 66 and 83, 132 and 110, 239 and 184, 808 and 584.  fp32 (8 + 2 heads, 32 sequences over 8,192):
+// 48 rows 175 and 199, 64 rows 225 and 202.
+constexpr int64_t SHARED_ROWS = 56;
 
 // What starting and ending a block costs, in keys, and the least share (that cost included) worth a workgroup and a merge.  Measured over
 // 32 ... 480 keys: one token over 1,100 keys 16.4 us with 64 (and 256), 14.8 with 240 (320); eight rollouts over a shared video 36.7
@@ -185,7 +195,7 @@ pa::PagedArgs arrange(const paged_attn_plan_t& plan, const void* q, int64_t q_st
   a.page_shift = plan.page_shift;
   a.scale = d.softmax_scale;
   const int64_t rows = (int64_t)num_tokens * plan.group;
-  a.shared_len = rows <= FEW_ROWS * num_seqs ? shared_len : nullptr;
+  a.shared_len = rows <= SHARED_ROWS * num_seqs ? shared_len : nullptr;
   a.blocks16 = blocks16_for(a.shared_len ? rows : (rows + num_seqs - 1) / num_seqs, d.dtype);
   a.groups = plan.num_cu;
   a.xcd_shift = plan.xcd_shift;
@@ -274,7 +284,7 @@ int paged_attn_plan(const paged_attn_desc_t* desc, paged_attn_plan_t** plan_out,
   }
   // What the shares leave of blocks that they cut, and, where shared keys are a segment of their own, partials of all rows.
   const int64_t block_rows = is_chunk(d.max_tokens * p->group, 1, d.dtype) ? pa::PAGED_CHUNK_ROWS : 64, slots = 2 * (int64_t)p->num_cu * block_rows;
-  const int64_t few = FEW_ROWS * d.max_seqs / p->group, tokens = few < d.max_tokens ? few : d.max_tokens;
+  const int64_t most = SHARED_ROWS * d.max_seqs / p->group, tokens = most < d.max_tokens ? most : d.max_tokens;
   size_t at = 256;
   auto take = [&](size_t bytes) {
     const size_t off = at;

@@ -228,7 +228,8 @@ def paged_attn_forward(plan: PagedAttnPlan, q, k_cache, v_cache, page_table, seq
                        shared_len=None, stream=None) -> None:
     """paged_attn_forward of the C ABI: attention of the new tokens q [T, Hq, D] over the pages of their sequences, into out
     [T, Hq, D] and lse_out [Hq, T] fp32 (or None).  The new tokens' keys and values are in the cache already (paged_kv_append).
-    shared_len: None, or an int32 tensor of one element: so many leading tokens of all sequences are in the same pages, which
-    calls of few rows then read once.  `workspace`: uint8, at least plan.workspace_bytes.  Enqueues only."""
+    shared_len: None, or an int32 tensor of one element: so many leading tokens of all sequences are in the same pages, which calls
+    of at most 56 rows (tokens times Hq / Hkv) a sequence then read once for every 64 rows (fp32: 32) of all sequences together.
+    `workspace`: uint8, at least plan.workspace_bytes.  Enqueues only."""
     _check("paged_attn_forward", (_native or _load_native()).attend(plan.handle, q, k_cache, v_cache, page_table, seq_lens, cu_new, out, lse_out,
                                                                     workspace, shared_len, _stream(stream)))

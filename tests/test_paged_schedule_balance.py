@@ -57,3 +57,15 @@ def test_numbers_beyond_32_bits_do_not_wrap():
         assert e.value.status == 2
     assert p.schedule_shape(8, 64) and p.schedule_shape(1, 1)
     p.destroy()
+
+
+@pytest.mark.parametrize("dtype,heads,new,shares", [
+    ("bf16", (28, 4), 1, True), ("bf16", (28, 4), 8, True), ("bf16", (28, 4), 9, False), ("bf16", (28, 4), 10, False),
+    ("bf16", (4, 4), 56, True), ("bf16", (4, 4), 57, False), ("f32", (8, 2), 14, True), ("f32", (8, 2), 16, False),
+])
+def test_shared_keys_are_a_segment_where_that_saves_passes(dtype, heads, new, shares):
+    """Up to 56 rows a sequence: fuller blocks of one sequence's rows lose more than they save (63 rows: 132 us shared, 110 not)."""
+    lens, cu = [9000 + 10 * i for i in range(8)], np.arange(9) * new
+    p = pa.paged_attn_plan(*heads, 128, 64, 100000, 150, 8, 8 * new, 0.1, dtype=dtype, device=-1)
+    assert (p.schedule(lens, cu, 8 * new, 8192)[:, 1] == -1).any() == shares
+    p.destroy()
