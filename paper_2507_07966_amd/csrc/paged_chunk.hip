@@ -1,8 +1,7 @@
 // Attention of new tokens over their pages for chunks (bf16): blocks of 256 stacked rows.
 //
 // Bound: bf16 MFMA.  A block is 256 rows m = i * group + (h % group) of one kv head and sequence, 32 a wavefront, two wavefronts a SIMD;
-// tiles of 64 keys go to LDS once for all of them, three of K and of V (four at D = 64, where a tile's work is shorter than a load's
-// latency), one barrier a tile.  Products, operand order and the
+// tiles of 64 keys go to LDS once for all of them, room for four of K and of V (one that is read, three under way), one barrier a tile.  Products, operand order and the
 // interleave of one tile's softmax with the product before are those of the prefill kernels (v_mfma_f32_16x16x32_bf16 on transposed
 // scores); what differs:
 //   - Keys come from pages.  A wavefront loads 8 rows of a tile; they lie in one page (page sizes are multiples of 16), whose
@@ -12,12 +11,15 @@
 //   - V is read transposed from row-major tiles (ds_read_b64_tr_b16): a paged cache has no images of its values.
 //   - The reference of the softmax is the maximum of a row's first tile, with no search afterwards; a tile's sum tells when some
 //     probability left the safe range.  Then the block is done again with its true maxima, which a pass over the
-//     scores alone finds first: one loop serves both, and no code that rescales accumulators takes registers from it.
+//     scores alone finds first: one loop serves both, and no code that rescales accumulators takes registers from it.  That pass has one
+//     tile under way at a time.  Where every block is done again (scores that grow by more than 11 along a sequence, or one key far above
+//     the others in its middle) a call takes 2.3 ... 2.4 times as long: 881 -> 2,140 us for the first call below, 139 -> 318 for the second.
 //   - A workgroup takes a share of the line of paged_sched.h: whole blocks, and parts of the two that its ends cut.
 //
 // Measured: the last 2,048 tokens of a sequence of 34,816 (28 + 4 heads of 128): 0.87 ... 0.92 ms, 1.1 PFLOP/s, the matrix pipe busy 54 %
-// of the cycles (the prefill kernels, whose values are stored as images, take 0.82).  24 chunks of 1 ... 301 tokens, 14 + 2 heads
-// of 64: 132 us, 0.65 PFLOP/s: 4.6 other vector instructions to an MFMA that is half as long (matrix pipe busy 30 %).  No LDS
+// of the cycles (the prefill kernels, whose values are stored as images, take 0.82).  24 chunks of 19 ... 294 tokens, 14 + 2 heads
+// of 64: 134 us, 0.65 PFLOP/s: 4.6 other vector instructions to an MFMA that is half as long, matrix pipe busy 30 %, wavefronts waiting
+// 32 %: 511 pieces, each of which begins with nothing under way.  No LDS
 // bank conflicts.  Loads issued between the MFMAs instead of at a tile's end: 905 ... 917 us (897); half of the wavefronts half a tile behind
 // the others, with a buffer more: 902 (874) and 147 (132); wave priorities make no difference.
 #include <hip/hip_runtime.h>

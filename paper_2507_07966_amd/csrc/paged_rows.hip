@@ -6,8 +6,10 @@
 //   - A workgroup takes shares of the line of paged_sched.h; a block is up to 16 NQ stacked rows (query heads of a GQA
 //     group, and new tokens), which all use every key that is loaded.
 //   - The 4 wavefronts split the KEYS of a tile, not the rows: a wavefront has its own 16 KiB stages in LDS, filled by direct-to-LDS
-//     loads (STAGES of them in flight or in use: 128 KiB a compute unit, which covers latency times rate), and
-//     waits for its own loads only; there is no barrier inside a block.  A page is looked up once for 16 keys (page
+//     loads (STAGES of them in flight or in use: 128 KiB a compute unit), and there is no barrier inside a block.  The
+//     kernel waits for the stage that it is about to read only, but the compiler, which knows of these loads and cannot tell the
+//     ring's places apart, adds a wait for all of them before every second stage in all but the two instances of heads of 64 and 16
+//     rows.  It also waits for them before the joint, which lies over the other wavefronts' rings.  A page is looked up once for 16 keys (page
 //     sizes are multiples of 16), in scalar registers one stage ahead; the loads' range ends at the last key or is empty where a page
 //     is missing, so LDS holds zeros there and nothing outside the cache is read.  A row that sees a key without a page, which is one whose
 //     limit is not below the smallest such key, becomes NaN at the end.
@@ -21,7 +23,8 @@
 // Measured (28 + 4 heads of 128, bf16): one token each of 64 sequences of 700 ... 17,000 keys, 1.08 GB of keys and values: 187 ... 193 us,
 // 5.6 ... 5.8 TB/s (15.4 ms in a kernel without direct-to-LDS loads, MFMA and equal shares).  8 rollouts over one video of 32,768 keys:
 // 27 us, of which 16 are its bytes; one sequence of 1,100 keys: 10.5 us: there latency counts, a chain of four reads to the
-// first key and the joint at the end.  fp32, chunks of 3 ... 130 tokens: 60 us, the matrix pipe about 83 % busy inside the loop.
+// first key and the joint at the end.  fp32, 5 chunks of 5 ... 106 tokens: 61 us, the matrix pipe busy 50 % of the cycles, 0.4
+// LDS bank conflicts a cycle of LDS use.
 // 8 wavefronts of one stage each instead of 4 of two: one token 16.5 (then 16.1) and fp32 83.6 us (72.9).
 #include <hip/hip_runtime.h>
 

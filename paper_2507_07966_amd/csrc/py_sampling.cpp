@@ -2,7 +2,7 @@
 //
 // A decode step's calls run for a few microseconds on the GPU, and the checks of ten tensors' types, shapes, devices and strides
 // take longer than that in Python (rope_axes_forward 12.1 us a call, paged_attn_forward 16.3 us, both bound by them); here they
-// take under one.  Every function returns None, or (status, text) of what it refuses; nothing has been enqueued then.
+// take 0.1 (0.4 with the call in Python; a name looked up in the package for every call, instead of once, adds 3.9).  Every function returns None, or (status, text) of what it refuses; nothing has been enqueued then.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

@@ -240,8 +240,10 @@ int launch(const RopeArgs& a, void* stream) {
   RopeKernelArgs k{};
   k.a = a;
   for (int i = 0; i < a.rope.rotary_dim / 2; ++i) k.axis_bits[i / 16] |= (uint32_t)a.rope.pair_axis[i] << (2 * (i % 16));
-  // As many heads as leave a few wavefronts to every SIMD: 8 from 2^21 units on (2^18 threads), 4 from 2^18 on.  In fp32, 5,377 tokens, 14 +
-  // 2 heads of 64 (2^20.6 units): 12.7 us with 4, 14.0 with 8; bf16, 18,432 tokens, 28 + 4 of 128 (2^22.2): 68.6 and 61.3.
+  // As many heads as leave a few wavefronts to every SIMD: 8 from 2^21 units on (2^18 threads), 4 from 2^18 on.  With 2, 4 and 8 heads, whole heads turned,
+  // bf16, 28 + 4 of 128: 2^17 units 5.2, 5.8, 7.3 us, 2^18 6.6, 6.5, 7.7, 2^19 10.5, 9.1, 7.7, 2^20 20, 15.9, 12.8, 2^21 37, 31, 28; fp32, 14 + 2 of 64:
+  // 2^18 4.0, 4.3, 5.2, 2^19 5.3, 5.3, 5.7, 2^20 7.8, 7.5, 6.4, 2^21 14.7, 13.0, 11.3.  Below 2^21 it depends: 46 of 64 channels turned in fp32
+  // (2^20.6 units) take 12.7 us with 4 and 14.0 with 8.
   const int64_t work = a.T * heads * units.count();
   const int hpt = work >= (1 << 21) ? 8 : work >= (1 << 18) ? 4 : 2;
   k.groups = (heads + hpt - 1) / hpt;
